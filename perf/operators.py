@@ -48,7 +48,7 @@ def listed():
 
 def _log(rng, lo, hi):
     """An integer whose logarithm is uniform over [lo, hi]."""
-    return max(lo, min(hi, int(round(lo * (hi / lo) ** rng.random()))))
+    return _other(max(lo, min(hi, int(round(lo * (hi / lo) ** rng.random())))))
 
 
 def _size(rng, lo, hi):
@@ -82,7 +82,7 @@ def draw(rng):
     most = 16384 * 2048 * 4096  # products of the largest listed case; a sixteenth of that in 32 bits
     while t * k * n * d > (most if kind != "f32" else most // 16) or e * n * d > 1 << 28 :
         t, n, d, e = max(1, t * 3 // 4), n if n <= d else n * 3 // 4, d if d < n else d * 3 // 4, max(4, e // 2) if e * n * d > 1 << 28 else e
-    return dict(op=op, E=e, k=k, T=t, N=_other(n), K=_other(d), type=kind, gather=rng.random() < 0.5, back=rng.random() < 0.5)
+    return dict(op=op, E=e, k=k, T=_other(t), N=_other(n), K=_other(d), type=kind, gather=rng.random() < 0.5, back=rng.random() < 0.5)
 
 
 # ---- inputs ----------------------------------------------------------------------------------------------------------------
