@@ -5,7 +5,9 @@
  * A tensor comprehension (arXiv 1802.04730, Section 3) is an index-notation
  * statement: every output element is a sum, over the indices that appear only
  * on the right-hand side, of a product of tensor accesses, optionally followed
- * by a pointwise epilogue.  This library evaluates six fixed comprehensions.
+ * by a pointwise epilogue.  This library evaluates six fixed comprehensions,
+ * and the operators around the experts of a language model (tc_embed to
+ * tc_expert_sum_grad, whose tensors may be of 16 bits) with their gradients.
  *
  * Conventions common to every entry point
  *  - Every tensor pointer is a DEVICE pointer to a dense row-major array (last
@@ -104,10 +106,17 @@ int64_t tc355_get_option(tc_option key);
  *   kron:   lds, tile, wave
  *   sconv:  i8, tile, split
  *   lut:    sum
+ *   embed, expert_sum, expert_sum_grad, route_grad: rows
+ *   embed_grad: small_sort, sort
+ *   route:  one, tiles
+ *   expert_mm, expert_mm_grad_x, expert_mm_grad_w: tile
  * A debugging and testing aid: tests pick the tolerance of the
  * arithmetic that actually ran instead of re-deriving the dispatch.
  */
 const char *tc355_last_path(void);
+
+/* Storage type of a tensor argument of the operators around experts (tc_embed ... tc_expert_sum_grad). */
+typedef enum { TC_F32 = 0, TC_BF16 = 1, TC_F16 = 2 } tc_type;
 
 /*
  * Transposed batched matmul (Section 7, "Transposed Batched Matrix
@@ -393,6 +402,161 @@ tc_status tc_sconv2d_infer(int64_t H, int64_t W, int64_t KH, int64_t KW,
 tc_status tc_lut(int32_t n_tables, const float *const *LUT,
                  const int32_t *const *Idx, float *const *O, const int64_t *E,
                  const int64_t *L, int64_t D, int64_t B, void *hip_stream);
+
+/*
+ * Operators around experts: a table of tokens, a router, the products of each
+ * expert's rows with its own weights, their weighted sum, and all gradients.
+ * Beside the conventions above:
+ *  - Matrices are of one storage type per call (tc_type): fp32, bfloat16 or
+ *    IEEE half.  Sums are kept in fp32 for the products and for 16-bit storage,
+ *    in fp64 where fp32 storage is only streamed (tc_embed, tc_embed_grad,
+ *    tc_expert_sum, tc_expert_sum_grad), and rounded once per output, to nearest even.  Weights of
+ *    the router are fp32, indices int32.
+ *  - Every result is the same each time: no sum depends on the order in which
+ *    workgroups run.
+ *  - Extents below 2^30 unless said otherwise (rows of the table: below
+ *    2^31 - 1); tensors may hold more than 2^31 elements.
+ *  - A pointer to an array without elements may be NULL.
+ *  - Indices and offsets live on the device, so the host cannot reject them.  Whatever they hold, nothing
+ *    outside the named arrays is read or written.
+ */
+
+/*
+ * Rows of a table of tokens, scaled:
+ *     O(t,j) = scale * LUT(Idx(t), j)              t < T, j < D
+ * LUT: [E,D]   Idx: [T] int32   O: [T,D], of LUT's type.
+ * An index outside [0, E) reads nothing and gives a row of NaN, as in tc_lut.
+ */
+tc_status tc_embed(const void *LUT, const int32_t *Idx, void *O, int64_t E,
+                   int64_t D, int64_t T, float scale, tc_type type,
+                   void *hip_stream);
+
+/*
+ * Gradient of tc_embed:
+ *     dLUT(e,j) (+)= scale * sum over the t with Idx(t) = e of dO(t,j)
+ * dO: [T,D]   dLUT: [E,D], of dO's type or fp32 (grad_type).
+ * Tokens are sorted by number first, equal ones in their order, so that each
+ * row's sum has one order.  Tokens with the number `pad` (-1: none) and with numbers
+ * outside [0, E) take no part.  add = 0: all of dLUT is written, with zeros where no
+ * token names the row; add = 1: the sum is added to what dLUT holds, and rows that no
+ * token names are not touched.
+ *   workspace  device scratch of at least tc_embed_grad_workspace_bytes(...)
+ *              bytes, 16-byte aligned (may be NULL for T = 0); contents on entry are irrelevant, calls that
+ *              share it must be ordered on one stream.
+ */
+size_t tc_embed_grad_workspace_bytes(int64_t E, int64_t D, int64_t T);
+tc_status tc_embed_grad(const void *dO, const int32_t *Idx, void *dLUT,
+                        int64_t E, int64_t D, int64_t T, float scale,
+                        int64_t pad, int32_t add, tc_type type,
+                        tc_type grad_type, void *workspace,
+                        size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Router: for every token the k largest of its E logits, their softmax weights,
+ * and the slots (t,i) in the experts' order.
+ * L: [T,E]   Wt: [T,k] fp32   Id: [T,k]   Off: [E+1]   Row: [T*k]   Place: [T,k]
+ *     Id(t,0..k-1)  the experts of the k largest logits, largest first, equal
+ *                   ones by the lower number
+ *     Wt(t,i)       exp(L(t,Id(t,i))) over the sum of exp(L(t,e)) over all e, or
+ *                   with norm = 1 over the k chosen only
+ *     Off(e)        number of slots of experts below e: expert e owns the places
+ *                   Off(e) .. Off(e+1)-1
+ *     Place(t,i)    the slot's place: slots by expert, those of one expert in
+ *                   order of (t,i)
+ *     Row(r)        the token of place r
+ * A logit of -inf is an expert that the token may not choose.  A slot that finds
+ * no other is left empty: Id = -1, Wt = 0, Place = -1; places from Off(E) on have Row = -1.  NaN ranks above
+ * every number; a token with a NaN or a +inf among its logits has weights of NaN
+ * (norm = 1: if one is among the chosen, which it is).
+ * 1 <= k <= E; E <= 1023 and k <= 64 (TC_ERR_UNSUPPORTED beyond).
+ *   workspace  device scratch of at least tc_route_workspace_bytes(...) bytes,
+ *              16-byte aligned; NULL where that is 0 (a few tokens).
+ */
+size_t tc_route_workspace_bytes(int64_t T, int64_t E, int64_t k);
+tc_status tc_route(const void *L, float *Wt, int32_t *Id, int32_t *Off,
+                   int32_t *Row, int32_t *Place, int64_t T, int64_t E,
+                   int64_t k, int32_t norm, tc_type type, void *workspace,
+                   size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Gradient of tc_route's weights:
+ *     dL(t,e) = [e = Id(t,i)] * Wt(t,i) * dWt(t,i) - S(t,e) * sum_i dWt(t,i) * Wt(t,i)
+ * with S = softmax(L(t,:)), or with norm = 1 the weight of a chosen expert and 0
+ * for the others.  L and Id as given to and by tc_route, dL: [T,E], of L's type.
+ * An Id outside [0, E) is an empty slot.  A number occurs once in a row of Id.
+ */
+tc_status tc_route_grad(const void *L, const int32_t *Id, const float *dWt,
+                        void *dL, int64_t T, int64_t E, int64_t k,
+                        int32_t norm, tc_type type, void *hip_stream);
+
+/*
+ * Products grouped by expert, ragged: for the rows r of expert e, Off(e) <= r < Off(e+1),
+ *     Y(r,n) = sum_k X(s(r),k) * W(e,n,k)        s(r) = Row(r), or r if Row is NULL
+ *     Y(r,n) = fmaxf(Y(r,n), 0)                  if relu
+ * X: [T,K] (T = R if Row is NULL)   W: [E,N,K]   Off: [E+1]   Row: [R] or NULL
+ * Y: [R,N].  Experts may own any number of rows, none among them.  Rows from Off(E) on (and
+ * below Off(0)) belong to no expert: from Off(E) on they are set to 0, below Off(0) not written.  Offsets are
+ * clamped to [0, R]; where they decrease, an expert owns nothing.  A Row outside [0, T) is a row of zeros.
+ * An fp32 sum over k is taken on the matrix core in blocks; NaN and Inf stay in the
+ * rows and columns that read them.  The clamp maps NaN and -0 to +0.
+ */
+tc_status tc_expert_mm(const void *X, const void *W, const int32_t *Off,
+                       const int32_t *Row, void *Y, int64_t T, int64_t R,
+                       int64_t E, int64_t N, int64_t K, int32_t relu,
+                       tc_type type, void *hip_stream);
+
+/*
+ * Gradient of tc_expert_mm with respect to its rows:
+ *     dX(r,k) = sum_n dY(r,n) * W(e,n,k)
+ *     dX(r,k) = 0 where gate is given and not gate(r,k) > 0
+ * dY: [R,N]   gate: [R,K] or NULL (the clamped output of the product before, which
+ * is this one's input)   dX: [R,K]; rows of no expert as in tc_expert_mm.  For a product that took its
+ * rows through Row, tc_expert_sum without weights adds dX's rows up by token.
+ */
+tc_status tc_expert_mm_grad_x(const void *dY, const void *W,
+                              const int32_t *Off, const void *gate, void *dX,
+                              int64_t R, int64_t E, int64_t N, int64_t K,
+                              tc_type type, void *hip_stream);
+
+/*
+ * Gradient of tc_expert_mm with respect to its weights:
+ *     dW(e,n,k) (+)= sum over the rows r of e of dY(r,n) * X(s(r),k)
+ * dW: [E,N,K], of dY's type or fp32 (grad_type); add = 1 adds to what it holds,
+ * add = 0 writes all of it, zeros for an expert without rows.
+ *   workspace  as in tc_tbmm_ws: device scratch of tc_expert_mm_grad_w_workspace_bytes(...)
+ *              bytes, 16-byte aligned; NULL or fewer bytes only cost time.
+ */
+size_t tc_expert_mm_grad_w_workspace_bytes(int64_t R, int64_t E, int64_t N,
+                                           int64_t K);
+tc_status tc_expert_mm_grad_w(const void *dY, const void *X,
+                              const int32_t *Off, const int32_t *Row, void *dW,
+                              int64_t T, int64_t R, int64_t E, int64_t N,
+                              int64_t K, int32_t add, tc_type type,
+                              tc_type grad_type, void *workspace,
+                              size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Weighted sum of the rows of a token's slots:
+ *     O(t,n) = sum_i Wt(t,i) * Y(Place(t,i), n)
+ * Y: [R,N]   Wt: [T,k] fp32, or NULL for ones   Place: [T,k]   O: [T,N].
+ * A Place outside [0, R) takes no part, nor does its weight; a token without
+ * places gives zeros.
+ */
+tc_status tc_expert_sum(const void *Y, const float *Wt, const int32_t *Place,
+                        void *O, int64_t T, int64_t R, int64_t k, int64_t N,
+                        tc_type type, void *hip_stream);
+
+/*
+ * Gradient of tc_expert_sum:
+ *     dY(Place(t,i), n) = Wt(t,i) * dO(t,n)
+ *     dWt(t,i)          = sum_n dO(t,n) * Y(Place(t,i), n)     (0 without a place)
+ * dO: [T,N]   dY: [R,N]   dWt: [T,k].  No place may occur twice.  Rows of dY
+ * that are no slot's place are not written.
+ */
+tc_status tc_expert_sum_grad(const void *dO, const void *Y, const float *Wt,
+                             const int32_t *Place, void *dY, float *dWt,
+                             int64_t T, int64_t R, int64_t k, int64_t N,
+                             tc_type type, void *hip_stream);
 
 #ifdef __cplusplus
 }

@@ -1,0 +1,250 @@
+// The router of a layer of experts.
+//   p = softmax(L(t,:));  the k largest logits of a token, equal ones by the lower number;  w = p there, or (norm) p over their sum
+//   Off, Row, Place: the slots (t,i) sorted by expert, stable; Off(e): the first place of expert e; Row(r): the token of place r;
+//   Place(t,i): the place of a slot
+//   dL(t,e) = [e chosen as i] w_i g_i - share_e * sum_i g_i w_i,  share = p, or (norm) w for the chosen and 0 for the others
+//
+// Logits of -inf are experts that a token may not choose: a slot that finds no other is left empty (number -1, weight 0, no place).
+// NaN ranks above every number, as does nothing else; a row with a NaN or a +inf has weights of NaN, as the formula has.
+// The selection compares the logits themselves, as integers that order as they do (-0 as +0), so that rounding never decides.
+//
+// A group of 16 lanes (64 for more than 128 experts) takes a token, each lane the logits lane, lane + G, ..: k rounds find the
+// largest of what is left by exchange inside the group.  What bounds it is those rounds' latency, not the logits' bytes.  A workgroup
+// takes ROUTE_TOKENS tokens and counts its slots per expert; a second launch sums the earlier workgroups' counts and places the
+// slots (key_sort.hpp's ranks by ballot).  Up to ROUTE_TOKENS tokens both are one launch.  No atomics on memory; integer ones in LDS.
+#pragma once
+#include "expert_types.hpp"
+#include "key_sort.hpp"
+
+namespace tc355 {
+
+constexpr int ROUTE_TOKENS = 64;      // of a workgroup
+constexpr int ROUTE_MOST_E = 1023;    // (with the empty slots' bin: 10 bits)
+constexpr int ROUTE_MOST_K = 64;
+constexpr int ROUTE_DIRECT_TILES = 256;
+
+struct RouteArgs {
+  const void* L;  // [T][E]
+  float* Wt;      // [T][k]
+  int* Id;        // [T][k]
+  int* Off;       // [E+1]
+  int* Row;       // [T*k]
+  int* Place;     // [T][k]
+  int* count;     // [tiles + 1][bins]; nullptr: one workgroup does it all
+  int T, E, k, norm, bits, tiles, summed;
+};
+
+__device__ __forceinline__ unsigned route_order(float x) {  // orders as the logits do; 0: -inf
+  if (x != x) return 0xffffffffu;
+  const unsigned b = __builtin_bit_cast(unsigned, x + 0.0f);
+  const unsigned o = b & 0x80000000u ? ~b : b | 0x80000000u;
+  return o - 0x007fffffu;  // (-inf is the lowest: 0x007fffff)
+}
+
+template <int G, typename F>
+__device__ __forceinline__ void group_all(F f) {
+#pragma unroll
+  for (int d = 1; d < G; d *= 2) f(d);
+}
+
+// The places of a workgroup's slots: Id of tokens t0 .. t0 + ROUTE_TOKENS, all threads.
+__device__ __forceinline__ void route_place(const RouteArgs& p, int tile, const int* start, int* count) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, bins = 1 << p.bits;
+  for (int b = lane; b < bins; b += 64) count[wave * bins + b] = 0;
+  const int64_t first = (int64_t)tile * ROUTE_TOKENS * p.k, all = (int64_t)p.T * p.k;
+  const int64_t last = min(first + (int64_t)ROUTE_TOKENS * p.k, all);
+  // a quarter of the slots for each wavefront, counted first, then placed
+  const int share = ((int)(last - first) + WAVES_PER_WG - 1) / WAVES_PER_WG;
+  const int64_t lo = min(first + (int64_t)wave * share, last), hi = min(lo + share, last);
+  for (int64_t s0 = lo; s0 < hi; s0 += 64) {
+    const bool on = s0 + lane < hi;
+    const int e = on ? p.Id[s0 + lane] : 0;
+    rank_and_count(count + wave * bins, e < 0 ? p.E : e, p.bits, on, lane);
+  }
+  __syncthreads();
+  for (int b = threadIdx.x; b < bins; b += WG_THREADS) {
+    int at = start[b];
+#pragma unroll
+    for (int w = 0; w < WAVES_PER_WG; w++) {
+      const int c = count[w * bins + b];
+      count[w * bins + b] = at;
+      at += c;
+    }
+  }
+  __syncthreads();
+  for (int64_t s0 = lo; s0 < hi; s0 += 64) {
+    const int64_t s = s0 + lane;
+    const bool on = s < hi;
+    const int e = on ? p.Id[s] : 0;
+    const int r = rank_and_count(count + wave * bins, e < 0 ? p.E : e, p.bits, on, lane);
+    if (on) {
+      p.Place[s] = e < 0 ? -1 : r;
+      p.Row[r] = e < 0 ? -1 : (int)(s / p.k);
+    }
+  }
+}
+
+template <typename T, int G, int V>
+__global__ __launch_bounds__(WG_THREADS) void route_kernel(RouteArgs p) {
+  extern __shared__ int mem[];  // [bins] counts; one workgroup: starts in their place, [waves][bins] counters behind
+  __shared__ int part[WAVES_PER_WG];
+  const int bins = 1 << p.bits;
+  for (int b = threadIdx.x; b < bins; b += WG_THREADS) mem[b] = 0;
+  __syncthreads();
+  const int lane = threadIdx.x & (G - 1), group = threadIdx.x / G;
+  const T* L = static_cast<const T*>(p.L);
+  for (int r = group; r < ROUTE_TOKENS; r += WG_THREADS / G) {
+    const int64_t t = (int64_t)blockIdx.x * ROUTE_TOKENS + r;
+    if (t >= p.T) break;  // (the whole group, and all groups behind it)
+    float x[V];
+    unsigned key[V];
+    float most = -__builtin_inff();
+#pragma unroll
+    for (int v = 0; v < V; v++) {
+      const int e = v * G + lane;
+      x[v] = e < p.E ? (float)L[t * p.E + e] : -__builtin_inff();
+      key[v] = route_order(x[v]);
+      most = fmaxf(most, x[v]);
+    }
+    group_all<G>([&](int d) { most = fmaxf(most, __shfl_xor(most, d)); });
+    if (most == -__builtin_inff()) most = 0.0f;  // (nothing to choose: every exp is 0, or NaN)
+    float sum = 0.0f;
+    if (!p.norm) {
+#pragma unroll
+      for (int v = 0; v < V; v++) sum += expf(x[v] - most);
+      group_all<G>([&](int d) { sum += __shfl_xor(sum, d); });
+    }
+    float val = 0.0f;
+    int id = -1;
+    const int slot_lane = lane;
+    for (int i = 0; i < p.k; i++) {
+      unsigned best = 0;
+      int at = 0x7fffffff;
+#pragma unroll
+      for (int v = 0; v < V; v++)
+        if (key[v] > best) {
+          best = key[v];
+          at = v * G + lane;
+        }
+      group_all<G>([&](int d) {
+        const unsigned ob = __shfl_xor(best, d);
+        const int oa = __shfl_xor(at, d);
+        if (ob > best || (ob == best && oa < at)) {
+          best = ob;
+          at = oa;
+        }
+      });
+      float mine = 0.0f;
+#pragma unroll
+      for (int v = 0; v < V; v++)
+        if (best && at == v * G + lane) {
+          key[v] = 0;
+          mine = x[v];
+        }
+      const float chosen = __shfl(mine, best ? at & (G - 1) : 0, G);
+      const float w = best ? expf(chosen - most) : 0.0f;
+      if (p.norm) sum += w;
+      if ((i & (G - 1)) == slot_lane) {
+        val = w;
+        id = best ? at : -1;
+      }
+      if ((i & (G - 1)) == G - 1 || i == p.k - 1) {  // (k <= G, by the host's choice of G)
+        const int s = (i & ~(G - 1)) + slot_lane;
+        if (s <= i) {
+          p.Wt[t * p.k + s] = id < 0 ? 0.0f : val / sum;
+          p.Id[t * p.k + s] = id;
+          atomicAdd(&mem[id < 0 ? p.E : id], 1);
+        }
+      }
+    }
+  }
+  __syncthreads();
+  if (p.count) {
+    for (int b = threadIdx.x; b < bins; b += WG_THREADS) p.count[(int64_t)blockIdx.x * bins + b] = mem[b];
+    return;
+  }
+  // one workgroup: counts to starts, then the places
+  __threadfence_block();
+  int run = 0;
+  for (int b0 = 0; b0 < bins; b0 += WG_THREADS) {
+    const int b = b0 + threadIdx.x, c = b < bins ? mem[b] : 0;
+    int total;
+    const int lower = block_prefix<WAVES_PER_WG>(c, part, &total);
+    if (b < bins) mem[b] = run + lower;
+    run += total;
+    if (b <= p.E) p.Off[b] = mem[b];
+  }
+  __syncthreads();
+  route_place(p, 0, mem, mem + bins);
+}
+
+static __global__ __launch_bounds__(WG_THREADS) void route_place_kernel(RouteArgs p) {
+  extern __shared__ int mem[];
+  __shared__ int part[WAVES_PER_WG];
+  const int bins = 1 << p.bits;
+  tile_starts<WG_THREADS>(p.count, p.tiles, bins, blockIdx.x, p.summed, mem, part);
+  if (blockIdx.x == 0)  // (before the first tile nothing counts: its starts are the experts')
+    for (int b = threadIdx.x; b <= p.E; b += WG_THREADS) p.Off[b] = mem[b];
+  route_place(p, blockIdx.x, mem, mem + bins);
+}
+
+struct RouteGradArgs {
+  const void* L;    // [T][E]
+  const int* Id;    // [T][k]
+  const float* dWt; // [T][k]
+  void* dL;         // [T][E]
+  int T, E, k, norm;
+};
+
+template <typename T, int G, int V>
+__global__ __launch_bounds__(WG_THREADS) void route_grad_kernel(RouteGradArgs p) {
+  const int lane = threadIdx.x & (G - 1);
+  const int64_t t = (int64_t)blockIdx.x * (WG_THREADS / G) + threadIdx.x / G;
+  if (t >= p.T) return;
+  const T* L = static_cast<const T*>(p.L) + t * p.E;
+  float x[V], g[V];
+  bool chosen[V];
+  float most = -__builtin_inff();
+#pragma unroll
+  for (int v = 0; v < V; v++) {
+    const int e = v * G + lane;
+    x[v] = e < p.E ? (float)L[e] : -__builtin_inff();
+    most = fmaxf(most, x[v]);
+    g[v] = 0.0f;
+    chosen[v] = false;
+  }
+  group_all<G>([&](int d) { most = fmaxf(most, __shfl_xor(most, d)); });
+  if (most == -__builtin_inff()) most = 0.0f;
+  for (int i = 0; i < p.k; i++) {
+    const int id = p.Id[t * p.k + i];
+    const float d = p.dWt[t * p.k + i];
+#pragma unroll
+    for (int v = 0; v < V; v++)
+      if (id == v * G + lane) {
+        g[v] = d;
+        chosen[v] = true;
+      }
+  }
+  float sum = 0.0f, inner = 0.0f;
+#pragma unroll
+  for (int v = 0; v < V; v++) {
+    x[v] = expf(x[v] - most);
+    if (!p.norm || chosen[v]) sum += x[v];
+    if (chosen[v]) inner += g[v] * x[v];
+  }
+  group_all<G>([&](int d) {
+    sum += __shfl_xor(sum, d);
+    inner += __shfl_xor(inner, d);
+  });
+  if (sum == 0.0f) sum = 1.0f;  // (a row of nothing, or without slots)
+  inner /= sum;
+#pragma unroll
+  for (int v = 0; v < V; v++) {
+    const int e = v * G + lane;
+    if (e >= p.E) continue;
+    const float share = !p.norm || chosen[v] ? x[v] / sum : 0.0f;
+    static_cast<T*>(p.dL)[t * p.E + e] = narrow<T>(share * ((chosen[v] ? g[v] : 0.0f) - inner));
+  }
+}
+
+}  // namespace tc355

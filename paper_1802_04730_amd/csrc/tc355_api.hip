@@ -720,6 +720,8 @@ bool try_gconv_i8_small(const GconvArgs& g, hipStream_t s, tc_status* st) {
 
 }  // namespace
 
+void tc355::note_path(const char* path) { t_path = path; }
+
 extern "C" {
 
 const char* tc_status_string(tc_status s) {

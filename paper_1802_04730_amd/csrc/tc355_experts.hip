@@ -1,0 +1,415 @@
+// Host side of the operators around experts: token tables, router, products grouped by expert, weighted sums, and their gradients
+// (include/tc355.h).  Argument validation, kernel selection and launches.
+#include "../../include/tc355.h"
+
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cstdint>
+#include <type_traits>
+
+#include "embed.hpp"
+#include "expert_mm.hpp"
+#include "expert_sum.hpp"
+#include "key_sort.hpp"
+#include "route.hpp"
+#include "tc355_host.hpp"
+
+using namespace tc355;
+
+namespace {
+
+constexpr int64_t kMostRows = (int64_t)1 << 30;   // rows, widths: 32-bit indices with room for a tile
+constexpr int64_t kMostIndex = ((int64_t)1 << 31) - 1;
+
+inline bool misaligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) != 0; }
+inline tc_status launched() { return hipGetLastError() == hipSuccess ? TC_OK : TC_ERR_LAUNCH; }
+inline tc_status took(const char* path, tc_status st) {
+  note_path(path);
+  return st;
+}
+inline bool known(tc_type t) { return t == TC_F32 || t == TC_BF16 || t == TC_F16; }
+inline int bits_of(int64_t v) {  // of a number up to v
+  int b = 1;
+  while (b < 62 && (v >> b)) b++;
+  return b;
+}
+inline int64_t round256(int64_t n) { return (n + 255) / 256 * 256; }
+
+// f(T{}) with the storage type
+template <typename F>
+tc_status by_type(tc_type t, F f) {
+  if (t == TC_F32) return f(float{});
+  if (t == TC_BF16) return f(bf16{});
+  return f(f16{});
+}
+
+// Lanes that share a row of `units` 16-byte units, and groups of them that a row takes.
+struct RowLanes {
+  int lpr, cols;
+};
+RowLanes row_lanes(int64_t width, int per16) {
+  const int64_t units = ceil_div(width, per16);
+  int lpr = 1;
+  while (lpr < units && lpr < 64) lpr *= 2;
+  return {lpr, (int)ceil_div(units, lpr)};
+}
+
+// ---- token tables -----------------------------------------------------------------------------------------------------------
+
+struct EmbedGradPlan {
+  int key_bits, passes, bits;
+  int64_t tiles, stretches;
+  int64_t key_a, order_a, key_b, order_b, count, part, bytes;  // offsets into the workspace
+};
+
+EmbedGradPlan embed_grad_plan(int64_t E, int64_t D, int64_t T) {
+  EmbedGradPlan p{};
+  p.key_bits = bits_of(E);
+  p.passes = (int)ceil_div(p.key_bits, SORT_MOST_BITS);
+  p.bits = (int)ceil_div(p.key_bits, p.passes);
+  p.tiles = ceil_div(T, SORT_TILE);
+  p.stretches = T / EMBED_RUN;
+  int64_t at = 0;
+  const auto take = [&](int64_t n) {
+    const int64_t o = at;
+    at += round256(n);
+    return o;
+  };
+  p.key_a = take(T * 4);
+  p.order_a = take(T * 4);
+  if (T > SORT_SMALL) {
+    p.key_b = take(T * 4);
+    p.order_b = take(T * 4);
+    p.count = take((p.tiles + 1) * ((int64_t)4 << p.bits));
+  }
+  p.part = take(p.stretches * D * 8);
+  p.bytes = at;
+  return p;
+}
+
+// The tokens sorted by number, for embed_grad; *key and *order: where they are.
+tc_status sort_tokens(const EmbedGradPlan& pl, const int32_t* Idx, int64_t T, int64_t E, int64_t pad, char* ws, const int** key, const int** order,
+                      hipStream_t s) {
+  int* keys[2] = {reinterpret_cast<int*>(ws + pl.key_a), reinterpret_cast<int*>(ws + pl.key_b)};
+  int* orders[2] = {reinterpret_cast<int*>(ws + pl.order_a), reinterpret_cast<int*>(ws + pl.order_b)};
+  SortPass a{};
+  a.n = (int)T;
+  a.E = (int)E;
+  a.bits = pl.bits;
+  a.pad = pad;
+  a.tiles = (int)pl.tiles;
+  a.key = Idx;
+  if (T <= SORT_SMALL) {
+    a.key_out = keys[0];
+    a.order_out = orders[0];
+    const size_t lds = (2 * (size_t)SORT_SMALL + 17 * ((size_t)1 << pl.bits)) * 4;
+    sort_small_kernel<<<1, 1024, lds, s>>>(a, pl.key_bits);
+    *key = keys[0];
+    *order = orders[0];
+    return launched();
+  }
+  a.count = reinterpret_cast<int*>(ws + pl.count);
+  a.summed = pl.tiles > SORT_DIRECT_TILES;
+  const unsigned tiles = (unsigned)pl.tiles, bins = 1u << pl.bits;
+  for (int i = 0; i < pl.passes; i++) {
+    a.shift = i * pl.bits;
+    a.key_out = keys[i & 1];
+    a.order_out = orders[i & 1];
+    sort_count_kernel<<<tiles, SORT_THREADS, 0, s>>>(a);
+    if (a.summed) sort_sum_kernel<<<(bins + 63) / 64, 64, 0, s>>>(a.count, (int)tiles, (int)bins);
+    sort_scatter_kernel<<<tiles, SORT_THREADS, 0, s>>>(a);
+    if (const tc_status st = launched(); st != TC_OK) return st;
+    a.key = keys[i & 1];
+    a.order = orders[i & 1];
+  }
+  *key = a.key;
+  *order = a.order;
+  return TC_OK;
+}
+
+// ---- router -----------------------------------------------------------------------------------------------------------------
+
+template <typename F>
+tc_status by_lanes(int64_t E, int64_t k, F f) {
+  typedef std::integral_constant<int, 16> G16;
+  typedef std::integral_constant<int, 64> G64;
+  if (k <= 16 && E <= 128) {
+    if (E <= 16) return f(G16{}, std::integral_constant<int, 1>{});
+    if (E <= 32) return f(G16{}, std::integral_constant<int, 2>{});
+    if (E <= 64) return f(G16{}, std::integral_constant<int, 4>{});
+    return f(G16{}, std::integral_constant<int, 8>{});
+  }
+  if (E <= 128) return f(G64{}, std::integral_constant<int, 2>{});
+  if (E <= 256) return f(G64{}, std::integral_constant<int, 4>{});
+  if (E <= 512) return f(G64{}, std::integral_constant<int, 8>{});
+  return f(G64{}, std::integral_constant<int, 16>{});
+}
+
+int64_t route_ws(int64_t T, int64_t E) {
+  const int64_t tiles = ceil_div(T, ROUTE_TOKENS);
+  return tiles <= 1 ? 0 : (tiles + 1) * ((int64_t)4 << bits_of(E));
+}
+
+// ---- products grouped by expert -----------------------------------------------------------------------------------------------
+
+// Row tiles that R rows of E experts can need, whatever their shares, those of no expert among them.
+int64_t most_row_tiles(int64_t R, int64_t E, int64_t bm) { return std::min(R, (R + (E + 1) * (bm - 1)) / bm); }
+
+template <typename T, bool ACROSS, bool ANY, int BM, int BN, int WM, int WN>
+tc_status launch_rows_tile(ExpertRowsArgs a, hipStream_t s) {
+  a.nt = (int)ceil_div(a.NO, BN);
+  const int64_t grid = (most_row_tiles(a.R, a.E, BM) * a.nt + 7) / 8 * 8;
+  if (grid > kMostIndex / (64 * WM * WN) * 2) return TC_ERR_UNSUPPORTED;
+  expert_rows_tile_kernel<T, ACROSS, ANY, BM, BN, WM, WN><<<dim3((unsigned)grid), dim3(64 * WM * WN), 0, s>>>(a);
+  return launched();
+}
+
+template <bool ACROSS>
+tc_status run_rows(const ExpertRowsArgs& a, tc_type type, hipStream_t s) {
+  return by_type(type, [&](auto t) {
+    typedef decltype(t) T;
+    const bool whole = (int64_t)a.Q * sizeof(T) % 16 == 0 && (!ACROSS || (int64_t)a.NO * sizeof(T) % 16 == 0);
+    return whole ? launch_rows_tile<T, ACROSS, false, 128, 128, 2, 2>(a, s) : launch_rows_tile<T, ACROSS, true, 128, 128, 2, 2>(a, s);
+  });
+}
+
+template <typename T, typename TO, bool ANY, int BM, int BN, int WM, int WN>
+tc_status launch_weights(ExpertWeightsArgs a, hipStream_t s) {
+  a.mt = (int)ceil_div(a.N, BM);
+  a.nt = (int)ceil_div(a.K, BN);
+  if (prod_reaches({a.mt, a.nt, a.E}, kMostIndex / (64 * WM * WN) * 2)) return TC_ERR_UNSUPPORTED;
+  const int64_t grid = ((int64_t)a.mt * a.nt * a.E + 7) / 8 * 8;
+  expert_weights_kernel<T, TO, ANY, BM, BN, WM, WN><<<dim3((unsigned)grid), dim3(64 * WM * WN), 0, s>>>(a);
+  return launched();
+}
+
+}  // namespace
+
+extern "C" {
+
+tc_status tc_embed(const void* LUT, const int32_t* Idx, void* O, int64_t E, int64_t D, int64_t T, float scale, tc_type type, void* hip_stream) {
+  if (!known(type) || E <= 0 || D <= 0 || T < 0) return TC_ERR_SHAPE;
+  if (!LUT || (T && (!Idx || !O))) return TC_ERR_NULL;
+  if (T && (O == LUT || O == static_cast<const void*>(Idx))) return TC_ERR_ALIAS;
+  if (misaligned(LUT) || misaligned(Idx) || misaligned(O)) return TC_ERR_ALIGN;
+  if (E > kMostIndex + 1 || D > kMostRows || T > kMostIndex) return TC_ERR_UNSUPPORTED;
+  if (T == 0) return TC_OK;
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  return took("embed:rows", by_type(type, [&](auto x) {
+                typedef decltype(x) X;
+                EmbedArgs a{LUT, Idx, O, E, T, (int)D, 0, 0, scale};
+                const RowLanes rl = row_lanes(D, Elem<X>::PER16);
+                a.lpr = rl.lpr;
+                a.cols = rl.cols;
+                const int64_t all = ceil_div(T * a.cols, WG_THREADS / a.lpr);
+                for (int64_t at = 0; at < all;) {
+                  const int64_t n = next_launch(all - at, WG_THREADS);
+                  embed_kernel<X><<<dim3((unsigned)n), dim3(WG_THREADS), 0, s>>>(a, at);
+                  at += n;
+                }
+                return launched();
+              }));
+}
+
+size_t tc_embed_grad_workspace_bytes(int64_t E, int64_t D, int64_t T) {
+  if (E <= 0 || D <= 0 || T <= 0 || E >= kMostIndex || D > kMostRows || T > kMostRows || prod_reaches({T, D}, (int64_t)1 << 59)) return 0;
+  return (size_t)embed_grad_plan(E, D, T).bytes;
+}
+
+tc_status tc_embed_grad(const void* dO, const int32_t* Idx, void* dLUT, int64_t E, int64_t D, int64_t T, float scale, int64_t pad, int32_t add, tc_type type,
+                        tc_type grad_type, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  if (!known(type) || (grad_type != type && grad_type != TC_F32) || E <= 0 || D <= 0 || T < 0) return TC_ERR_SHAPE;
+  if (!dLUT || (T && (!dO || !Idx))) return TC_ERR_NULL;
+  if (T && (dLUT == dO || dLUT == static_cast<const void*>(Idx))) return TC_ERR_ALIAS;
+  if (workspace && (workspace == dO || workspace == static_cast<const void*>(Idx) || workspace == dLUT)) return TC_ERR_ALIAS;
+  if (misaligned(dO) || misaligned(Idx) || misaligned(dLUT)) return TC_ERR_ALIGN;
+  if (E >= kMostIndex || D > kMostRows || T > kMostRows || prod_reaches({std::max<int64_t>(T, 1), D}, (int64_t)1 << 59)) return TC_ERR_UNSUPPORTED;
+  const EmbedGradPlan pl = embed_grad_plan(E, D, T);
+  if (T && (!workspace || misaligned(workspace) || workspace_bytes < (size_t)pl.bytes)) return TC_ERR_WORKSPACE;
+  if (T == 0 && add) return TC_OK;
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  char* ws = static_cast<char*>(workspace);
+  return by_type(type, [&](auto x) {
+    typedef decltype(x) X;
+    EmbedGradArgs a{};
+    const RowLanes rl = row_lanes(D, Elem<X>::PER16);
+    a.dO = dO; a.dLUT = dLUT; a.part = T ? ws + pl.part : nullptr;
+    a.T = (int)T; a.E = (int)E; a.D = (int)D; a.lpr = rl.lpr; a.cols = rl.cols; a.scale = scale; a.add = add != 0;
+    const int groups = WG_THREADS / a.lpr;
+    const int64_t stretch_grid = ceil_div(pl.stretches * a.cols, groups);
+    if (stretch_grid > kMostIndex / WG_THREADS * 2) return TC_ERR_UNSUPPORTED;
+    // rows of a workgroup: enough that its bisections are few beside its rows, as long as 2048 workgroups are left
+    int rows = 64;
+    while (rows > 1 && ceil_div(E, rows) < 2048) rows /= 2;
+    a.rows = rows;
+    if (T) {
+      const tc_status st = sort_tokens(pl, Idx, T, E, pad, ws, &a.key, &a.order, s);
+      if (st != TC_OK) return st;
+      if (stretch_grid) embed_stretch_kernel<X><<<dim3((unsigned)stretch_grid), dim3(WG_THREADS), 0, s>>>(a, (int)pl.stretches);
+    }
+    const dim3 grid((unsigned)ceil_div(E, rows));
+    if (grad_type == TC_F32) embed_grad_kernel<X, float><<<grid, dim3(WG_THREADS), 0, s>>>(a);
+    else embed_grad_kernel<X, X><<<grid, dim3(WG_THREADS), 0, s>>>(a);
+    return took(T <= SORT_SMALL ? "embed_grad:small_sort" : "embed_grad:sort", launched());
+  });
+}
+
+size_t tc_route_workspace_bytes(int64_t T, int64_t E, int64_t k) {
+  if (T <= 0 || E <= 0 || k <= 0 || k > E || E > ROUTE_MOST_E || k > ROUTE_MOST_K || prod_reaches({T, k}, kMostRows)) return 0;
+  return (size_t)route_ws(T, E);
+}
+
+tc_status tc_route(const void* L, float* Wt, int32_t* Id, int32_t* Off, int32_t* Row, int32_t* Place, int64_t T, int64_t E, int64_t k, int32_t norm,
+                   tc_type type, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  if (!known(type) || T < 0 || E <= 0 || k <= 0 || k > E) return TC_ERR_SHAPE;
+  if (!Off || (T && (!L || !Wt || !Id || !Row || !Place))) return TC_ERR_NULL;
+  const void* out[] = {Wt, Id, Off, Row, Place, workspace};
+  for (int i = 0; i < 6; i++) {
+    if (out[i] && out[i] == L) return TC_ERR_ALIAS;
+    for (int j = 0; j < i; j++)
+      if (out[i] && out[i] == out[j]) return TC_ERR_ALIAS;
+    if (i < 5 && misaligned(out[i])) return TC_ERR_ALIGN;
+  }
+  if (misaligned(L)) return TC_ERR_ALIGN;
+  if (E > ROUTE_MOST_E || k > ROUTE_MOST_K || prod_reaches({std::max<int64_t>(T, 1), k}, kMostRows) || T > kMostRows) return TC_ERR_UNSUPPORTED;
+  const int64_t need = route_ws(T, E);
+  if (need && (!workspace || misaligned(workspace) || workspace_bytes < (size_t)need)) return TC_ERR_WORKSPACE;
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  RouteArgs a{L, Wt, Id, Off, Row, Place, need ? static_cast<int*>(workspace) : nullptr, (int)T, (int)E, (int)k, norm != 0, bits_of(E),
+              (int)std::max<int64_t>(1, ceil_div(T, ROUTE_TOKENS)), 0};
+  a.summed = a.tiles > ROUTE_DIRECT_TILES;
+  const size_t bins = (size_t)4 << a.bits;
+  return by_type(type, [&](auto x) {
+    return by_lanes(E, k, [&](auto g, auto v) {
+      typedef decltype(x) X;
+      route_kernel<X, g.value, v.value><<<dim3((unsigned)a.tiles), dim3(WG_THREADS), a.count ? bins : bins * (1 + WAVES_PER_WG), s>>>(a);
+      if (!a.count) return took("route:one", launched());
+      if (a.summed) sort_sum_kernel<<<dim3(((1u << a.bits) + 63) / 64), dim3(64), 0, s>>>(a.count, a.tiles, 1 << a.bits);
+      route_place_kernel<<<dim3((unsigned)a.tiles), dim3(WG_THREADS), bins * (1 + WAVES_PER_WG), s>>>(a);
+      return took("route:tiles", launched());
+    });
+  });
+}
+
+tc_status tc_route_grad(const void* L, const int32_t* Id, const float* dWt, void* dL, int64_t T, int64_t E, int64_t k, int32_t norm, tc_type type,
+                        void* hip_stream) {
+  if (!known(type) || T < 0 || E <= 0 || k <= 0 || k > E) return TC_ERR_SHAPE;
+  if (T && (!L || !Id || !dWt || !dL)) return TC_ERR_NULL;
+  if (T && (dL == L || dL == static_cast<const void*>(Id) || dL == static_cast<const void*>(dWt))) return TC_ERR_ALIAS;
+  if (misaligned(L) || misaligned(Id) || misaligned(dWt) || misaligned(dL)) return TC_ERR_ALIGN;
+  if (E > ROUTE_MOST_E || k > ROUTE_MOST_K || prod_reaches({std::max<int64_t>(T, 1), k}, kMostRows)) return TC_ERR_UNSUPPORTED;
+  if (T == 0) return TC_OK;
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  const RouteGradArgs a{L, Id, dWt, dL, (int)T, (int)E, (int)k, norm != 0};
+  return by_type(type, [&](auto x) {
+    return by_lanes(E, 1, [&](auto g, auto v) {
+      typedef decltype(x) X;
+      const int64_t grid = ceil_div(T, WG_THREADS / g.value);
+      if (grid > kMostIndex / WG_THREADS * 2) return TC_ERR_UNSUPPORTED;
+      route_grad_kernel<X, g.value, v.value><<<dim3((unsigned)grid), dim3(WG_THREADS), 0, s>>>(a);
+      return took("route_grad:rows", launched());
+    });
+  });
+}
+
+tc_status tc_expert_mm(const void* X, const void* W, const int32_t* Off, const int32_t* Row, void* Y, int64_t T, int64_t R, int64_t E, int64_t N, int64_t K,
+                       int32_t relu, tc_type type, void* hip_stream) {
+  if (!known(type) || T < 0 || R < 0 || E <= 0 || N <= 0 || K <= 0 || (!Row && T != R)) return TC_ERR_SHAPE;
+  if (!W || !Off || (R && (!Y || (T && !X)))) return TC_ERR_NULL;
+  if (R && (Y == X || Y == W || Y == static_cast<const void*>(Off) || Y == static_cast<const void*>(Row))) return TC_ERR_ALIAS;
+  if (misaligned(X) || misaligned(W) || misaligned(Off) || misaligned(Row) || misaligned(Y)) return TC_ERR_ALIGN;
+  if (T >= kMostRows || R >= kMostRows || E >= kMostRows || N >= kMostRows || K >= kMostRows) return TC_ERR_UNSUPPORTED;
+  if (R == 0) return TC_OK;
+  const ExpertRowsArgs a{X, W, Y, nullptr, Off, Row, (int)R, (int)T, (int)E, (int)K, (int)N, 0, relu != 0};
+  return took("expert_mm:tile", run_rows<false>(a, type, static_cast<hipStream_t>(hip_stream)));
+}
+
+tc_status tc_expert_mm_grad_x(const void* dY, const void* W, const int32_t* Off, const void* gate, void* dX, int64_t R, int64_t E, int64_t N, int64_t K,
+                              tc_type type, void* hip_stream) {
+  if (!known(type) || R < 0 || E <= 0 || N <= 0 || K <= 0) return TC_ERR_SHAPE;
+  if (!W || !Off || (R && (!dY || !dX))) return TC_ERR_NULL;
+  if (R && (dX == dY || dX == W || dX == static_cast<const void*>(Off) || dX == gate)) return TC_ERR_ALIAS;
+  if (misaligned(dY) || misaligned(W) || misaligned(Off) || misaligned(gate) || misaligned(dX)) return TC_ERR_ALIGN;
+  if (R >= kMostRows || E >= kMostRows || N >= kMostRows || K >= kMostRows) return TC_ERR_UNSUPPORTED;
+  if (R == 0) return TC_OK;
+  const ExpertRowsArgs a{dY, W, dX, gate, Off, nullptr, (int)R, (int)R, (int)E, (int)N, (int)K, 0, 0};
+  return took("expert_mm_grad_x:tile", run_rows<true>(a, type, static_cast<hipStream_t>(hip_stream)));
+}
+
+size_t tc_expert_mm_grad_w_workspace_bytes(int64_t R, int64_t E, int64_t N, int64_t K) {
+  (void)R; (void)E; (void)N; (void)K;
+  return 0;
+}
+
+tc_status tc_expert_mm_grad_w(const void* dY, const void* X, const int32_t* Off, const int32_t* Row, void* dW, int64_t T, int64_t R, int64_t E, int64_t N,
+                              int64_t K, int32_t add, tc_type type, tc_type grad_type, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  (void)workspace_bytes;
+  if (!known(type) || (grad_type != type && grad_type != TC_F32) || T < 0 || R < 0 || E <= 0 || N <= 0 || K <= 0 || (!Row && T != R)) return TC_ERR_SHAPE;
+  if (!Off || !dW || (R && (!dY || (T && !X)))) return TC_ERR_NULL;
+  if (dW == dY || dW == X || dW == static_cast<const void*>(Off) || dW == static_cast<const void*>(Row)) return TC_ERR_ALIAS;
+  if (workspace && (workspace == dY || workspace == X || workspace == dW || workspace == static_cast<const void*>(Off) || workspace == static_cast<const void*>(Row)))
+    return TC_ERR_ALIAS;
+  if (misaligned(dY) || misaligned(X) || misaligned(Off) || misaligned(Row) || misaligned(dW) || misaligned(workspace)) return TC_ERR_ALIGN;
+  if (T >= kMostRows || R >= kMostRows || E >= kMostRows || N >= kMostRows || K >= kMostRows) return TC_ERR_UNSUPPORTED;
+  if (R == 0 && add) return TC_OK;
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  ExpertWeightsArgs a{dY, X, dW, Off, Row, (int)R, (int)T, (int)E, (int)N, (int)K, 0, 0, add != 0};
+  return took("expert_mm_grad_w:tile", by_type(type, [&](auto t) {
+                typedef decltype(t) T_;
+                const bool whole = N * (int64_t)sizeof(T_) % 16 == 0 && K * (int64_t)sizeof(T_) % 16 == 0;
+                if (grad_type == TC_F32)
+                  return whole ? launch_weights<T_, float, false, 128, 128, 2, 2>(a, s) : launch_weights<T_, float, true, 128, 128, 2, 2>(a, s);
+                return whole ? launch_weights<T_, T_, false, 128, 128, 2, 2>(a, s) : launch_weights<T_, T_, true, 128, 128, 2, 2>(a, s);
+              }));
+}
+
+tc_status tc_expert_sum(const void* Y, const float* Wt, const int32_t* Place, void* O, int64_t T, int64_t R, int64_t k, int64_t N, tc_type type,
+                        void* hip_stream) {
+  if (!known(type) || T < 0 || R < 0 || k <= 0 || N <= 0) return TC_ERR_SHAPE;
+  if (T && (!Place || !O || (R && !Y))) return TC_ERR_NULL;
+  if (T && (O == Y || O == static_cast<const void*>(Wt) || O == static_cast<const void*>(Place))) return TC_ERR_ALIAS;
+  if (misaligned(Y) || misaligned(Wt) || misaligned(Place) || misaligned(O)) return TC_ERR_ALIGN;
+  if (T > kMostRows || R > kMostRows || N > kMostRows || k > kMostRows) return TC_ERR_UNSUPPORTED;
+  if (T == 0) return TC_OK;
+  return took("expert_sum:rows", by_type(type, [&](auto x) {
+                typedef decltype(x) X;
+                ExpertSumArgs a{Y, Wt, Place, O, T, R, (int)N, (int)k, 0, 0};
+                const RowLanes rl = row_lanes(N, Elem<X>::PER16);
+                a.lpr = rl.lpr;
+                a.cols = rl.cols;
+                const int64_t grid = ceil_div(T * a.cols, WG_THREADS / a.lpr);
+                if (grid > kMostIndex / WG_THREADS * 2) return TC_ERR_UNSUPPORTED;
+                expert_sum_kernel<X><<<dim3((unsigned)grid), dim3(WG_THREADS), 0, static_cast<hipStream_t>(hip_stream)>>>(a);
+                return launched();
+              }));
+}
+
+tc_status tc_expert_sum_grad(const void* dO, const void* Y, const float* Wt, const int32_t* Place, void* dY, float* dWt, int64_t T, int64_t R, int64_t k,
+                             int64_t N, tc_type type, void* hip_stream) {
+  if (!known(type) || T < 0 || R < 0 || k <= 0 || N <= 0) return TC_ERR_SHAPE;
+  if (T && (!dO || !Wt || !Place || !dWt || (R && (!Y || !dY)))) return TC_ERR_NULL;
+  const void* in[] = {dO, Y, Wt, Place};
+  for (const void* i : in) {
+    if (i && (dY == i || dWt == i)) return TC_ERR_ALIAS;
+    if (misaligned(i)) return TC_ERR_ALIGN;
+  }
+  if (dY && dY == static_cast<const void*>(dWt)) return TC_ERR_ALIAS;
+  if (misaligned(dY) || misaligned(dWt)) return TC_ERR_ALIGN;
+  if (T > kMostRows || R > kMostRows || N > kMostRows || k > kMostRows) return TC_ERR_UNSUPPORTED;
+  if (T == 0) return TC_OK;
+  return took("expert_sum_grad:rows", by_type(type, [&](auto x) {
+                typedef decltype(x) X;
+                const ExpertSumGradArgs a{dO, Y, Wt, Place, dY, dWt, T, R, (int)N, (int)k};
+                const int64_t grid = ceil_div(T, WAVES_PER_WG);
+                if (grid > kMostIndex / WG_THREADS * 2) return TC_ERR_UNSUPPORTED;
+                const dim3 g((unsigned)grid), b(WG_THREADS);
+                hipStream_t s = static_cast<hipStream_t>(hip_stream);
+                if (k <= 2) expert_sum_grad_kernel<X, 2><<<g, b, 0, s>>>(a);
+                else if (k <= 4) expert_sum_grad_kernel<X, 4><<<g, b, 0, s>>>(a);
+                else expert_sum_grad_kernel<X, 8><<<g, b, 0, s>>>(a);
+                return launched();
+              }));
+}
+
+}  // extern "C"

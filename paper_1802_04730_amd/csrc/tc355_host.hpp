@@ -5,6 +5,9 @@
 
 namespace tc355 {
 
+// Sets what tc355_last_path returns on this thread (a string that lives on); in tc355_api.hip.
+void note_path(const char* path);
+
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // True if the product of the (positive) extents reaches `limit`; never overflows: it stops at the first factor

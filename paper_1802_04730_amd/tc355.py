@@ -33,10 +33,16 @@ TC_MLP_STATIC_SCRATCH_BYTES = 8 << 20
 TC_OPT_INT8, TC_OPT_MLP_KERNEL, TC_OPT_MLP_SPIN_LIMIT = 0, 1, 2
 TC_INT8_AUTO, TC_INT8_OFF, TC_INT8_TEN, TC_INT8_THIRTEEN = 0, 1, 2, 3
 TC_MLP_AUTO, TC_MLP_ROWS, TC_MLP_TILES, TC_MLP_PER_LAYER = 0, 1, 2, 3
+# storage types of the operators around experts (tc_type)
+TC_F32, TC_BF16, TC_F16 = 0, 1, 2
+_TYPES = {torch.float32: TC_F32, torch.bfloat16: TC_BF16, torch.float16: TC_F16}
 
 EXPORTS = ["tc_status_string", "tc355_version", "tc355_set_option", "tc355_get_option", "tc355_last_path", "tc_tbmm", "tc_tbmm_ws", "tc_tbmm_workspace_bytes", "tc_mlp_fcrelu", "tc_mlp_fcrelu_workspace_bytes",
            "tc_mlp_fcrelu_static",
-           "tc_group_conv", "tc_group_conv_infer", "tc_kron", "tc_sconv2d", "tc_sconv2d_infer", "tc_lut"]
+           "tc_group_conv", "tc_group_conv_infer", "tc_kron", "tc_sconv2d", "tc_sconv2d_infer", "tc_lut",
+           "tc_embed", "tc_embed_grad", "tc_embed_grad_workspace_bytes", "tc_route", "tc_route_workspace_bytes", "tc_route_grad",
+           "tc_expert_mm", "tc_expert_mm_grad_x", "tc_expert_mm_grad_w", "tc_expert_mm_grad_w_workspace_bytes", "tc_expert_sum",
+           "tc_expert_sum_grad"]
 
 
 _RAW_STREAM = getattr(torch._C, "_cuda_getCurrentRawStream", None)
@@ -90,6 +96,21 @@ def lib() -> ctypes.CDLL:
     L.tc_sconv2d_infer.restype = ctypes.c_int
     L.tc_lut.argtypes = [i32, vp, vp, vp, vp, vp, i64, i64, vp]
     L.tc_lut.restype = ctypes.c_int
+    size, f32, kind = ctypes.c_size_t, ctypes.c_float, ctypes.c_int
+    for name, args in {"tc_embed": [vp, vp, vp, i64, i64, i64, f32, kind, vp],
+                       "tc_embed_grad": [vp, vp, vp, i64, i64, i64, f32, i64, i32, kind, kind, vp, size, vp],
+                       "tc_route": [vp] * 6 + [i64, i64, i64, i32, kind, vp, size, vp],
+                       "tc_route_grad": [vp] * 4 + [i64, i64, i64, i32, kind, vp],
+                       "tc_expert_mm": [vp] * 5 + [i64] * 5 + [i32, kind, vp],
+                       "tc_expert_mm_grad_x": [vp] * 5 + [i64] * 4 + [kind, vp],
+                       "tc_expert_mm_grad_w": [vp] * 5 + [i64] * 5 + [i32, kind, kind, vp, size, vp],
+                       "tc_expert_sum": [vp] * 4 + [i64] * 4 + [kind, vp],
+                       "tc_expert_sum_grad": [vp] * 6 + [i64] * 4 + [kind, vp]}.items():
+        getattr(L, name).argtypes = args
+        getattr(L, name).restype = ctypes.c_int
+    for name, n in (("tc_embed_grad_workspace_bytes", 3), ("tc_route_workspace_bytes", 3), ("tc_expert_mm_grad_w_workspace_bytes", 4)):
+        getattr(L, name).argtypes = [i64] * n
+        getattr(L, name).restype = size
     _load_fast(L)
     _LIB = L
     return L
@@ -360,3 +381,134 @@ def tc_lut(LUT, Idx, O, stream=None) -> None:
     Ev = _array([x.shape[0] for x in LUT], n)
     Lv = _array([x.shape[1] for x in Idx], n)
     _check(lib().tc_lut(n, Lp, Ip, Op, Ev, Lv, D, B, _stream(stream)), "tc_lut")
+
+
+# ---- operators around experts --------------------------------------------------------------------------------------------------
+
+
+def _typed(t, name: str, dims: int, dtype=None):
+    """Address of a dense CUDA tensor of `dims` dimensions, of one of the storage types or of `dtype`."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError("%s must be a torch CUDA tensor" % name)
+    if (t.dtype is not dtype) if dtype is not None else (t.dtype not in _TYPES):
+        raise TypeError("%s must be %s, got %s" % (name, dtype or "float32, bfloat16 or float16", t.dtype))
+    if t.dim() != dims:
+        raise ValueError("%s must have %d dimensions" % (name, dims))
+    if not t.is_contiguous():
+        raise ValueError("%s must be dense row-major (contiguous)" % name)
+    return t.data_ptr()
+
+
+def _fit(ok: bool, where: str) -> None:
+    if not ok:
+        raise ValueError("%s: shapes do not fit" % where)
+
+
+def _workspace(ws):
+    if ws is None:
+        return None, 0
+    if not isinstance(ws, torch.Tensor) or not ws.is_cuda or not ws.is_contiguous():
+        raise TypeError("workspace must be a contiguous CUDA tensor")
+    return ws.data_ptr(), ws.numel() * ws.element_size()
+
+
+def tc_embed(LUT, Idx, O, scale: float = 1.0, stream=None) -> None:
+    """O[T,D] = scale * LUT[Idx[T], :] (int32 numbers; one outside [0, E) gives a row of NaN)."""
+    l, i, o = _typed(LUT, "LUT", 2), _typed(Idx, "Idx", 1, torch.int32), _typed(O, "O", 2, LUT.dtype)
+    (E, D), T = LUT.shape, Idx.shape[0]
+    _fit(tuple(O.shape) == (T, D), "tc_embed")
+    _check(lib().tc_embed(l, i, o, E, D, T, scale, _TYPES[LUT.dtype], _stream(stream)), "tc_embed")
+
+
+def tc_embed_grad_workspace_bytes(E: int, D: int, T: int) -> int:
+    return int(lib().tc_embed_grad_workspace_bytes(int(E), int(D), int(T)))
+
+
+def tc_embed_grad(dO, Idx, dLUT, workspace, scale: float = 1.0, pad: int = -1, add: bool = False, stream=None) -> None:
+    """dLUT[E,D] (+)= scale * the sum of the rows of dO[T,D] whose number Idx[T] is the row's; `pad` and numbers outside [0, E) take no part.
+
+    dLUT is of dO's type or float32.  ``workspace``: a uint8 tensor of at least tc_embed_grad_workspace_bytes(E, D, T) bytes."""
+    d, i, g = _typed(dO, "dO", 2), _typed(Idx, "Idx", 1, torch.int32), _typed(dLUT, "dLUT", 2, None if dLUT.dtype is torch.float32 else dO.dtype)
+    (T, D), E = dO.shape, dLUT.shape[0]
+    _fit(dLUT.shape[1] == D and Idx.shape[0] == T, "tc_embed_grad")
+    wp, wn = _workspace(workspace)
+    _check(lib().tc_embed_grad(d, i, g, E, D, T, scale, pad, int(add), _TYPES[dO.dtype], _TYPES[dLUT.dtype], wp, wn, _stream(stream)), "tc_embed_grad")
+
+
+def tc_route_workspace_bytes(T: int, E: int, k: int) -> int:
+    return int(lib().tc_route_workspace_bytes(int(T), int(E), int(k)))
+
+
+def tc_route(L, Wt, Id, Off, Row, Place, workspace=None, norm: bool = False, stream=None) -> None:
+    """Weights Wt[T,k] and numbers Id[T,k] of the k largest of L[T,E], and the slots by expert: Off[E+1], Row[T*k], Place[T,k].
+
+    ``workspace``: a uint8 tensor of at least tc_route_workspace_bytes(T, E, k) bytes (None only when that is 0)."""
+    i32 = torch.int32
+    args = (_typed(L, "L", 2), _typed(Wt, "Wt", 2, torch.float32), _typed(Id, "Id", 2, i32), _typed(Off, "Off", 1, i32), _typed(Row, "Row", 1, i32),
+            _typed(Place, "Place", 2, i32))
+    (T, E), k = L.shape, Id.shape[1]
+    _fit(tuple(Id.shape) == tuple(Wt.shape) == tuple(Place.shape) == (T, k) and Off.shape[0] == E + 1 and Row.shape[0] == T * k, "tc_route")
+    wp, wn = _workspace(workspace)
+    _check(lib().tc_route(*args, T, E, k, int(norm), _TYPES[L.dtype], wp, wn, _stream(stream)), "tc_route")
+
+
+def tc_route_grad(L, Id, dWt, dL, norm: bool = False, stream=None) -> None:
+    """dL[T,E]: the gradient of tc_route's weights, from L[T,E], Id[T,k] and dWt[T,k]."""
+    args = (_typed(L, "L", 2), _typed(Id, "Id", 2, torch.int32), _typed(dWt, "dWt", 2, torch.float32), _typed(dL, "dL", 2, L.dtype))
+    (T, E), k = L.shape, Id.shape[1]
+    _fit(tuple(Id.shape) == tuple(dWt.shape) == (T, k) and dL.shape == L.shape, "tc_route_grad")
+    _check(lib().tc_route_grad(*args, T, E, k, int(norm), _TYPES[L.dtype], _stream(stream)), "tc_route_grad")
+
+
+def tc_expert_mm(X, W, Off, Row, Y, relu: bool = False, stream=None) -> None:
+    """Y[R,N]: rows Off[e] .. Off[e+1] are those of X times W[e] ([N,K]), clamped at 0 if relu; row r of X[T,K] is Row[r], or r where Row is None."""
+    i32 = torch.int32
+    args = (_typed(X, "X", 2), _typed(W, "W", 3, X.dtype), _typed(Off, "Off", 1, i32), None if Row is None else _typed(Row, "Row", 1, i32),
+            _typed(Y, "Y", 2, X.dtype))
+    (T, K), (E, N), R = X.shape, W.shape[:2], Y.shape[0]
+    _fit(W.shape[2] == K and Off.shape[0] == E + 1 and Y.shape[1] == N and (T if Row is None else Row.shape[0]) == R, "tc_expert_mm")
+    _check(lib().tc_expert_mm(*args, T, R, E, N, K, int(relu), _TYPES[X.dtype], _stream(stream)), "tc_expert_mm")
+
+
+def tc_expert_mm_grad_x(dY, W, Off, gate, dX, stream=None) -> None:
+    """dX[R,K]: the rows of each expert of dY[R,N] times W[e] ([N,K]); 0 where gate[R,K] (or None) is not above 0."""
+    args = (_typed(dY, "dY", 2), _typed(W, "W", 3, dY.dtype), _typed(Off, "Off", 1, torch.int32), None if gate is None else _typed(gate, "gate", 2, dY.dtype),
+            _typed(dX, "dX", 2, dY.dtype))
+    (R, N), (E, N2, K) = dY.shape, W.shape
+    _fit(N == N2 and Off.shape[0] == E + 1 and tuple(dX.shape) == (R, K) and (gate is None or tuple(gate.shape) == (R, K)), "tc_expert_mm_grad_x")
+    _check(lib().tc_expert_mm_grad_x(*args, R, E, N, K, _TYPES[dY.dtype], _stream(stream)), "tc_expert_mm_grad_x")
+
+
+def tc_expert_mm_grad_w_workspace_bytes(R: int, E: int, N: int, K: int) -> int:
+    return int(lib().tc_expert_mm_grad_w_workspace_bytes(int(R), int(E), int(N), int(K)))
+
+
+def tc_expert_mm_grad_w(dY, X, Off, Row, dW, workspace=None, add: bool = False, stream=None) -> None:
+    """dW[E,N,K] (+)= for each expert the products of its rows of dY[R,N] with those of X (taken through Row as in tc_expert_mm).
+
+    dW is of dY's type or float32.  ``workspace``: as tc_tbmm_ws; less than tc_expert_mm_grad_w_workspace_bytes(R, E, N, K) bytes
+    only cost time."""
+    i32 = torch.int32
+    args = (_typed(dY, "dY", 2), _typed(X, "X", 2, dY.dtype), _typed(Off, "Off", 1, i32), None if Row is None else _typed(Row, "Row", 1, i32),
+            _typed(dW, "dW", 3, None if dW.dtype is torch.float32 else dY.dtype))
+    (R, N), (T, K), E = dY.shape, X.shape, dW.shape[0]
+    _fit(tuple(dW.shape) == (E, N, K) and Off.shape[0] == E + 1 and (T if Row is None else Row.shape[0]) == R, "tc_expert_mm_grad_w")
+    wp, wn = _workspace(workspace)
+    _check(lib().tc_expert_mm_grad_w(*args, T, R, E, N, K, int(add), _TYPES[dY.dtype], _TYPES[dW.dtype], wp, wn, _stream(stream)), "tc_expert_mm_grad_w")
+
+
+def tc_expert_sum(Y, Wt, Place, O, stream=None) -> None:
+    """O[T,N] = the sum over i of Wt[T,k] (None: ones) times the rows Place[T,k] of Y[R,N]; a place outside [0, R) takes no part."""
+    args = (_typed(Y, "Y", 2), None if Wt is None else _typed(Wt, "Wt", 2, torch.float32), _typed(Place, "Place", 2, torch.int32), _typed(O, "O", 2, Y.dtype))
+    (R, N), (T, k) = Y.shape, Place.shape
+    _fit(tuple(O.shape) == (T, N) and (Wt is None or tuple(Wt.shape) == (T, k)), "tc_expert_sum")
+    _check(lib().tc_expert_sum(*args, T, R, k, N, _TYPES[Y.dtype], _stream(stream)), "tc_expert_sum")
+
+
+def tc_expert_sum_grad(dO, Y, Wt, Place, dY, dWt, stream=None) -> None:
+    """dY[R,N] (rows of the places that occur) and dWt[T,k]: the gradients of tc_expert_sum, from dO[T,N]."""
+    args = (_typed(dO, "dO", 2), _typed(Y, "Y", 2, dO.dtype), _typed(Wt, "Wt", 2, torch.float32), _typed(Place, "Place", 2, torch.int32),
+            _typed(dY, "dY", 2, dO.dtype), _typed(dWt, "dWt", 2, torch.float32))
+    (R, N), (T, k) = Y.shape, Place.shape
+    _fit(tuple(dO.shape) == (T, N) and tuple(Wt.shape) == tuple(dWt.shape) == (T, k) and dY.shape == Y.shape, "tc_expert_sum_grad")
+    _check(lib().tc_expert_sum_grad(*args, T, R, k, N, _TYPES[dO.dtype], _stream(stream)), "tc_expert_sum_grad")

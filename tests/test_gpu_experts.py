@@ -1,0 +1,539 @@
+"""The operators around experts on the GPU against the float64 oracle.
+
+Tolerances, before any run: an output is a sum of n terms kept in (at least) 32 bits and rounded once to the storage type, so it is
+off by at most  u(type) |ref| + 2 (n + 4) 2^-24 sum|terms|  plus the type's smallest step near zero; u = 2^-24, 2^-8, 2^-11 for
+float32, bfloat16, float16.  Exponentials add 2^-21 relative to a weight.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import experts as ref
+from paper_1802_04730_amd import tc355 as tc
+
+pytestmark = pytest.mark.gpu
+
+TYPES = [torch.float32, torch.bfloat16, torch.float16]
+UNIT = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
+STEP = {torch.float32: 2.0 ** -126, torch.bfloat16: 2.0 ** -126, torch.float16: 2.0 ** -24}
+
+
+def _rand(shape, dtype, seed, std=1.0):
+    return (torch.from_numpy(np.random.default_rng(seed).standard_normal(shape).astype(np.float32)) * std).to(dtype).cuda()
+
+
+def _np(t):
+    return None if t is None else (t.double() if t.is_floating_point() else t.long()).cpu().numpy()
+
+
+def _ints(a):
+    return torch.from_numpy(np.ascontiguousarray(a, dtype=np.int32)).cuda()
+
+
+def _close(got, want, mag, n, dtype, what=""):
+    g = _np(got)
+    assert g.shape == want.shape, what
+    tol = UNIT[dtype] * np.abs(want) + 2 * (n + 4) * 2.0 ** -24 * mag + STEP[dtype]
+    bad = ~(np.abs(g - want) <= tol)
+    assert not bad.any(), "%s: %d of %d off, worst %g over its tolerance" % (what, bad.sum(), bad.size, np.nanmax(np.where(bad, np.abs(g - want) / tol, 0)))
+
+
+def _bytes(n):
+    return torch.empty(n, dtype=torch.uint8, device="cuda") if n else None
+
+
+# ---- token tables -----------------------------------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("E,D,T", [(1, 1, 1), (7, 3, 5), (100, 8, 1), (50, 17, 33), (1000, 64, 300), (300, 513, 70), (20, 1000, 40), (33, 4099, 9)])
+def test_embed(dtype, E, D, T):
+    LUT = _rand((E, D), dtype, 1)
+    Idx = np.random.default_rng(2).integers(-1, E + 1, T)
+    O = torch.empty((T, D), dtype=dtype, device="cuda")
+    tc.tc_embed(LUT, _ints(Idx), O, 1.7)
+    want = ref.embed(_np(LUT), Idx, np.float32(1.7).astype(np.float64))
+    got = _np(O)
+    assert np.array_equal(np.isnan(got), np.isnan(want))
+    ok = ~np.isnan(want)
+    assert (np.abs(got - want)[ok] <= (UNIT[dtype] * np.abs(want) + 2.0 ** -24 * np.abs(want) + STEP[dtype])[ok]).all()
+
+
+def _grad(dtype, grad, E, D, T, add, Idx, pad, seed=3):
+    dO = _rand((T, D), dtype, seed)
+    dLUT = _rand((E, D), grad, seed + 1) if add else torch.full((E, D), float("nan"), dtype=grad, device="cuda")
+    there = _np(dLUT) if add else None
+    tc.tc_embed_grad(dO, _ints(Idx), dLUT, _bytes(tc.tc_embed_grad_workspace_bytes(E, D, T)), 0.3, pad, add)
+    want, mag = ref.embed_grad(_np(dO), Idx, E, np.float32(0.3).astype(np.float64), pad, there)
+    most = np.bincount(Idx[(Idx >= 0) & (Idx < E)], minlength=1).max() if T else 0
+    _close(dLUT, want, mag, most, grad)
+    return dO, dLUT
+
+
+@pytest.mark.parametrize("dtype,grad", [(d, g) for d in TYPES for g in {d, torch.float32}])
+@pytest.mark.parametrize("E,D,T", [(1, 1, 1), (1, 5, 300), (7, 3, 5), (3, 64, 700), (900, 33, 31), (50, 520, 400), (3000, 8, 4096), (300, 12, 4097), (70, 20, 9000)])
+@pytest.mark.parametrize("add", [False, True])
+def test_embed_grad(dtype, grad, E, D, T, add):
+    rng = np.random.default_rng(E + T)
+    Idx = np.minimum((rng.random(T) ** 3 * (E + 2)).astype(np.int64) - 1, E)  # a few numbers often; -1 and E among them
+    _grad(dtype, grad, E, D, T, add, Idx, pad=int(E // 2))
+
+
+@pytest.mark.parametrize("T", [64, 32 * 40, 5000])
+def test_embed_grad_of_one_number_and_of_none(T):
+    for value in (2, 4, -7):  # a row, the pad, outside
+        _grad(torch.bfloat16, torch.float32, 5, 24, T, False, np.full(T, value), pad=4)
+
+
+def test_embed_grad_of_many_tokens_and_of_a_long_table():
+    rng = np.random.default_rng(5)
+    _grad(torch.float32, torch.float32, 1000, 4, 140001, False, rng.integers(0, 1000, 140001), pad=-1)  # counts summed by a launch of their own
+    _grad(torch.bfloat16, torch.bfloat16, (1 << 21) + 3, 2, 5000, False, rng.integers(0, (1 << 21) + 3, 5000), pad=-1)  # three digits
+
+
+def test_embed_grad_without_tokens():
+    for add in (False, True):
+        g = torch.full((5, 3), 2.0, device="cuda")
+        tc.tc_embed_grad(torch.empty((0, 3), device="cuda"), _ints([]), g, None, add=add)
+        assert bool((g == (2.0 if add else 0.0)).all())
+
+
+def test_embed_grad_is_the_same_each_time():
+    Idx = np.random.default_rng(6).integers(0, 9, 6000)
+    a, b = (_grad(torch.float32, torch.float32, 9, 40, 6000, False, Idx, -1)[1] for _ in range(2))
+    assert torch.equal(a, b)
+
+
+def test_tables_beyond_32_bit_offsets():
+    E, D = (1 << 20) + 7, 4096  # 4.3e9 elements
+    LUT = torch.empty((E, D), dtype=torch.bfloat16, device="cuda")
+    at = np.array([0, 1 << 19, E - 1, (1 << 20) + 1])
+    rows = _rand((4, D), torch.bfloat16, 8)
+    LUT[torch.from_numpy(at).cuda()] = rows
+    O = torch.empty((4, D), dtype=torch.bfloat16, device="cuda")
+    tc.tc_embed(LUT, _ints(at), O)
+    assert torch.equal(O, rows)
+    tc.tc_embed_grad(rows, _ints(at), LUT, _bytes(tc.tc_embed_grad_workspace_bytes(E, D, 4)))
+    assert torch.equal(LUT[torch.from_numpy(at).cuda()], rows)
+    LUT[torch.from_numpy(at).cuda()] = 0
+    assert not bool(LUT.view(torch.int32).any())
+
+
+# ---- router -----------------------------------------------------------------------------------------------------------------
+
+
+def _route(L, k, norm):
+    T, E = L.shape
+    i32 = dict(dtype=torch.int32, device="cuda")
+    out = [torch.full((T, k), float("nan"), device="cuda"), torch.full((T, k), 77, **i32), torch.full((E + 1,), 77, **i32), torch.full((T * k,), 77, **i32),
+           torch.full((T, k), 77, **i32)]
+    tc.tc_route(L, *out, _bytes(tc.tc_route_workspace_bytes(T, E, k)), norm)
+    return out
+
+
+def _check_route(L, k, norm):
+    out, want = _route(L, k, norm), ref.route(_np(L), k, norm)
+    for name, g, w in zip(("Id", "Off", "Row", "Place"), out[1:], want[1:]):
+        assert np.array_equal(_np(g), w), name
+    g, w = _np(out[0]), want[0]
+    assert np.array_equal(np.isnan(g), np.isnan(w))
+    ok = ~np.isnan(w)
+    E = L.shape[1]
+    assert (np.abs(g - w)[ok] <= ((2.0 ** -21 + (E + 4) * 2.0 ** -23) * w + 2.0 ** -126)[ok]).all()
+    return out
+
+
+def _logits(T, E, dtype, seed, std=2.0):
+    L = _rand((T, E), dtype, seed, std)
+    rng = np.random.default_rng(seed)
+    L[torch.from_numpy(rng.random((T, E)) < 0.1).cuda()] = float("-inf")
+    L[torch.from_numpy(rng.random(T) < 0.1).cuda()] = float("-inf")
+    L[torch.from_numpy(rng.random((T, E)) < 0.1).cuda()] = 0.5  # (ties)
+    return L
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("norm", [False, True])
+@pytest.mark.parametrize("T,E,k", [(1, 1, 1), (1, 8, 2), (5, 3, 3), (64, 16, 4), (65, 17, 5), (130, 32, 1), (70, 33, 8), (200, 64, 6), (90, 128, 16), (67, 129, 8),
+                                   (40, 100, 20), (66, 256, 64), (20, 300, 17), (30, 1023, 9), (300, 5, 2)])
+def test_route(dtype, norm, T, E, k):
+    _check_route(_logits(T, E, dtype, T * E + k), k, norm)
+
+
+def test_route_of_many_tokens():
+    _check_route(_logits(64 * 30 + 1, 8, torch.bfloat16, 1), 3, True)
+    L = _logits(64 * 257, 4, torch.float32, 2)  # counts summed by a launch of their own
+    out = _route(L, 2, False)
+    Id, Off, Row, Place = (_np(x) for x in out[1:])
+    key = np.where(Id < 0, 4, Id).ravel()
+    order = np.argsort(key, kind="stable")
+    assert np.array_equal(Off, np.concatenate([[0], np.cumsum(np.bincount(key, minlength=5)[:4])]))
+    there = np.arange(len(order)) < Off[4]
+    assert np.array_equal(Row, np.where(there, order // 2, -1))
+    place = np.empty(len(order), np.int64)
+    place[order] = np.where(there, np.arange(len(order)), -1)
+    assert np.array_equal(Place.ravel(), place)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("norm", [False, True])
+def test_route_of_special_logits(dtype, norm):
+    low, nan, inf = torch.finfo(dtype).min, float("nan"), float("inf")
+    L = torch.tensor([[-inf] * 5, [low] * 5, [low, -inf, low, -inf, -inf], [nan, 1, 2, 3, 4], [1, inf, 2, 0, 0], [0.0, -0.0, 0.0, -0.0, 0.0], [-0.0, 0.0, -1, -inf, low],
+                      [nan] * 5, [nan, -inf, -inf, -inf, -inf], [inf, inf, -inf, 3, nan], [torch.finfo(dtype).max, low, 0, 0, 0]], dtype=dtype).cuda()
+    for k in (1, 3, 5):
+        _check_route(L, k, norm)
+
+
+def test_route_without_tokens():
+    out = _route(torch.empty((0, 6), device="cuda"), 2, False)
+    assert not bool(out[2].any())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("norm", [False, True])
+@pytest.mark.parametrize("T,E,k", [(1, 1, 1), (9, 8, 2), (33, 17, 5), (20, 64, 16), (21, 130, 20), (5, 1023, 3)])
+def test_route_grad(dtype, norm, T, E, k):
+    L = _logits(T, E, dtype, T + E)
+    Id = _route(L, k, norm)[1]
+    dWt = _rand((T, k), torch.float32, 4)
+    dL = torch.full((T, E), float("nan"), dtype=dtype, device="cuda")
+    tc.tc_route_grad(L, Id, dWt, dL, norm)
+    want = ref.route_grad(_np(L), _np(Id), _np(dWt), norm)
+    big = np.abs(_np(dWt)).max()  # |dL| terms: weights at most 1, times dWt
+    got = _np(dL)
+    assert (np.abs(got - want) <= UNIT[dtype] * np.abs(want) + (2.0 ** -20 + (E + 16) * 2.0 ** -22) * big + STEP[dtype]).all()
+
+
+@pytest.mark.parametrize("norm", [False, True])
+def test_route_grad_by_differences(norm):
+    """Central differences of sum(dWt * Wt) in 64 bits, the chosen experts held: off by about h^2 times the third derivative (at most |dWt|)."""
+    T, E, k, h = 6, 9, 3, 1e-4
+    L = _rand((T, E), torch.float32, 12)
+    Id, dWt = _route(L, k, norm)[1], _rand((T, k), torch.float32, 13)
+    dL = torch.empty_like(L)
+    tc.tc_route_grad(L, Id, dWt, dL, norm)
+    L0, ids, g = _np(L), _np(Id), _np(dWt)
+
+    def loss(x):
+        p = np.take_along_axis(ref.softmax_rows(x), ids, 1)
+        return (g * (p / p.sum(1, keepdims=True) if norm else p)).sum()
+
+    for t, e in np.ndindex(T, E):
+        up, down = L0.copy(), L0.copy()
+        up[t, e] += h
+        down[t, e] -= h
+        assert abs((loss(up) - loss(down)) / (2 * h) - _np(dL)[t, e]) < 1e-5
+
+
+# ---- products grouped by expert ------------------------------------------------------------------------------------------------
+
+
+def _offsets(E, R, seed, kind):
+    """Offsets of E experts over at most R rows: uneven with empty ones, all rows of one, none at all, none left over."""
+    rng = np.random.default_rng(seed)
+    if kind == "one":
+        off = np.where(np.arange(E + 1) > E // 2, R, 0)
+    elif kind == "none":
+        off = np.zeros(E + 1)
+    else:
+        cuts = np.sort(rng.integers(0, R + 1, E))
+        off = np.concatenate([[0], cuts])
+        if kind == "all":
+            off[-1] = R
+    return off.astype(np.int64)
+
+
+MM_SHAPES = [(1, 1, 1, 1, 1), (3, 5, 2, 7, 9), (20, 40, 4, 64, 64), (50, 30, 3, 130, 72), (300, 410, 5, 136, 200), (60, 150, 70, 24, 40), (33, 64, 9, 129, 257),
+             (128, 256, 2, 128, 64), (513, 513, 1, 257, 96), (16, 32, 8, 512, 1000), (7, 14, 130, 48, 33), (40, 260, 2, 8, 1500)]  # T, R, E, N, K
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,R,E,N,K", MM_SHAPES)
+@pytest.mark.parametrize("kind", ["some", "all", "one", "none"])
+def test_expert_mm(dtype, T, R, E, N, K, kind):
+    rng = np.random.default_rng(R + E)
+    Off = _offsets(E, R, R, kind)
+    W = _rand((E, N, K), dtype, 1, K ** -0.5)
+    for gather in (False, True):
+        X = _rand((T if gather else R, K), dtype, 2)
+        Row = rng.integers(-1, T + 1, R) if gather else None  # (a row outside is one of zeros)
+        for relu in (False, True):
+            Y = torch.full((R, N), float("nan"), dtype=dtype, device="cuda")
+            tc.tc_expert_mm(X, W, _ints(Off), None if Row is None else _ints(Row), Y, relu)
+            want, mag = ref.expert_mm(_np(X), _np(W), Off, Row, R, relu)
+            _close(Y, want, mag, K, dtype, tc.last_path())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,R,E,N,K", MM_SHAPES)
+@pytest.mark.parametrize("kind", ["some", "all", "one", "none"])
+def test_expert_mm_grads(dtype, T, R, E, N, K, kind):
+    rng = np.random.default_rng(R + E + 1)
+    Off = _offsets(E, R, R + 1, kind)
+    W, dY = _rand((E, N, K), dtype, 3, K ** -0.5), _rand((R, N), dtype, 4)
+    gate = _rand((R, K), dtype, 5)
+    for g in (None, gate):
+        dX = torch.full((R, K), float("nan"), dtype=dtype, device="cuda")
+        tc.tc_expert_mm_grad_x(dY, W, _ints(Off), g, dX)
+        want, mag = ref.expert_mm_grad_x(_np(dY), _np(W), Off, _np(g))
+        _close(dX, want, mag, N, dtype, tc.last_path())
+    ws = _bytes(tc.tc_expert_mm_grad_w_workspace_bytes(R, E, N, K))
+    for gather, grad, add, w in ((False, dtype, False, ws), (True, torch.float32, True, ws), (True, dtype, True, None)):
+        X = _rand((T if gather else R, K), dtype, 6)
+        Row = rng.integers(-1, T + 1, R) if gather else None
+        dW = _rand((E, N, K), grad, 7) if add else torch.full((E, N, K), float("nan"), dtype=grad, device="cuda")
+        there = _np(dW) if add else None
+        tc.tc_expert_mm_grad_w(dY, X, _ints(Off), None if Row is None else _ints(Row), dW, w, add)
+        want, mag = ref.expert_mm_grad_w(_np(dY), _np(X), Off, Row, there)
+        _close(dW, want, mag, R, grad, tc.last_path())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_what_an_expert_does_not_read_does_not_matter(dtype):
+    """Inf and NaN in rows of no expert, in other experts' rows and weights; in an expert's own they stay in their rows and columns."""
+    R, E, N, K = 300, 4, 72, 88
+    Off = np.array([0, 130, 130, 200, 290])
+    X, W, dY = _rand((R, K), dtype, 1), _rand((E, N, K), dtype, 2), _rand((R, N), dtype, 3)
+    X[290:], dY[290:], W[1] = float("nan"), float("inf"), float("nan")
+    X[140:150, 3], dY[250:255, 7] = float("inf"), float("nan")
+    Y, dX, dW = torch.empty((R, N), dtype=dtype, device="cuda"), torch.empty((R, K), dtype=dtype, device="cuda"), torch.empty((E, N, K), dtype=dtype, device="cuda")
+    off = _ints(Off)
+    tc.tc_expert_mm(X, W, off, None, Y)
+    tc.tc_expert_mm_grad_x(dY, W, off, None, dX)
+    tc.tc_expert_mm_grad_w(dY, X, off, None, dW)
+    y, dx, dw = (torch.isfinite(t) for t in (Y, dX, dW))
+    assert not bool(y[140:150].any()) and bool(y[:140].all()) and bool(y[150:].all()) and not bool(Y[290:].any())
+    assert not bool(dx[250:255].any()) and bool(dx[:250].all()) and bool(dx[255:].all()) and not bool(dX[290:].any())
+    assert not bool(dw[2, :, 3].any()) and not bool(dw[3, 7].any()) and not bool(dW[1].any())
+    dw[2, :, 3], dw[3, 7] = True, True
+    assert bool(dw.all())
+
+
+def test_offsets_that_make_no_sense_stay_inside():
+    R, E, N, K = 70, 3, 40, 48
+    X, W = _rand((R, K), torch.bfloat16, 1), _rand((E, N, K), torch.bfloat16, 2)
+    for off in ([0, 50, 20, 500], [-9, -3, 10, 2 ** 31 - 1], [5, 4, 3, 2], [2 ** 31 - 1, -2 ** 31, 0, 70]):
+        big = [torch.full((R + 64, n), 7.0, dtype=torch.bfloat16, device="cuda") for n in (N, K)]
+        dW = torch.empty((E, N, K), dtype=torch.bfloat16, device="cuda")
+        tc.tc_expert_mm(X, W, _ints(off), None, big[0][:R])
+        tc.tc_expert_mm_grad_x(big[0][:R], W, _ints(off), None, big[1][:R])
+        tc.tc_expert_mm_grad_w(big[0][:R], X, _ints(off), None, dW)
+        assert all(bool((b[R:] == 7.0).all()) for b in big)
+
+
+def test_products_of_no_rows():
+    W, off = _rand((3, 8, 16), torch.float32, 1), _ints([0, 0, 0, 0])
+    e = lambda *s: torch.empty(s, device="cuda")  # noqa: E731
+    tc.tc_expert_mm(e(0, 16), W, off, None, e(0, 8))
+    tc.tc_expert_mm_grad_x(e(0, 8), W, off, None, e(0, 16))
+    for add in (False, True):
+        dW = torch.full((3, 8, 16), 3.0, device="cuda")
+        tc.tc_expert_mm_grad_w(e(0, 8), e(0, 16), off, None, dW, add=add)
+        assert bool((dW == (3.0 if add else 0.0)).all())
+
+
+def test_weights_beyond_32_bit_offsets():
+    E, N, K, R = 9, 16384, 16384, 40  # 2.4e9 elements, 4.8 GB
+    W = torch.zeros((E, N, K), dtype=torch.bfloat16, device="cuda")
+    W[8, ::1000] = _rand((17, K), torch.bfloat16, 1, K ** -0.5)
+    X, Off = _rand((R, K), torch.bfloat16, 2), np.array([0, 4] + [20] * 7 + [38])
+    Y = torch.empty((R, N), dtype=torch.bfloat16, device="cuda")
+    tc.tc_expert_mm(X, W, _ints(Off), None, Y)
+    x, w = _np(X), _np(W[8, ::1000])
+    _close(Y[20:38, ::1000], x[20:38] @ w.T, np.abs(x[20:38]) @ np.abs(w.T), K, torch.bfloat16)
+    Y[20:38, ::1000] = 0
+    assert not bool(Y.any())
+    dY = torch.zeros((R, N), dtype=torch.bfloat16, device="cuda")
+    dY[30, 16000], dY[1, 5] = 2.0, 1.0
+    dX = torch.empty((R, K), dtype=torch.bfloat16, device="cuda")
+    tc.tc_expert_mm_grad_x(dY, W, _ints(Off), None, dX)
+    assert torch.equal(dX[30], W[8, 16000] * 2) and not bool(dX[:30].any()) and not bool(dX[31:].any())
+    tc.tc_expert_mm_grad_w(dY, X, _ints(Off), None, W)
+    assert torch.equal(W[8, 16000], X[30] * 2) and torch.equal(W[0, 5], X[1])
+    W[8, 16000], W[0, 5] = 0, 0
+    assert not bool(W.view(torch.int32).any())
+
+
+# ---- weighted sums ------------------------------------------------------------------------------------------------------------
+
+
+def _places(T, k, R, seed):
+    """Every place at most once; some slots without one, some outside."""
+    rng = np.random.default_rng(seed)
+    P = rng.permutation(max(R, T * k))[:T * k].reshape(T, k)
+    return np.where((P >= R) | (rng.random((T, k)) < 0.1), rng.choice([-1, R, -2 ** 31], (T, k)), P)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,k,N", [(1, 1, 1), (3, 2, 7), (20, 4, 64), (9, 3, 515), (50, 8, 40), (5, 9, 33), (4, 20, 1030), (130, 1, 8)])
+def test_expert_sum(dtype, T, k, N):
+    R = T * k
+    P = _places(T, k, R, T + k)
+    Y, Wt, dO = _rand((R, N), dtype, 1), _rand((T, k), torch.float32, 2), _rand((T, N), dtype, 3)
+    for w in (Wt, None):
+        O = torch.full((T, N), float("nan"), dtype=dtype, device="cuda")
+        tc.tc_expert_sum(Y, w, _ints(P), O)
+        want, mag = ref.expert_sum(_np(Y), _np(w), P)
+        _close(O, want, mag, k, dtype)
+    dY, dWt = torch.full((R, N), 5.0, dtype=dtype, device="cuda"), torch.full((T, k), float("nan"), device="cuda")
+    tc.tc_expert_sum_grad(dO, Y, Wt, _ints(P), dY, dWt)
+    wdY, wdWt, mag = ref.expert_sum_grad(_np(dO), _np(Y), _np(Wt), P, np.full((R, N), 5.0))
+    _close(dY, wdY, np.abs(wdY), 1, dtype)
+    _close(dWt, wdWt, mag, N, torch.float32)
+
+
+def test_sums_skip_what_has_no_place():
+    Y = torch.full((4, 16), float("nan"), device="cuda")
+    Y[2] = 3.0
+    Wt = torch.tensor([[float("nan"), 2.0], [float("inf"), float("nan")]], device="cuda")
+    P, O = _ints([[-1, 2], [-1, -1]]), torch.empty((2, 16), device="cuda")
+    tc.tc_expert_sum(Y, Wt, P, O)
+    assert bool((O[0] == 6.0).all()) and not bool(O[1].any())
+    dY, dWt = torch.zeros_like(Y), torch.empty_like(Wt)
+    tc.tc_expert_sum_grad(torch.ones((2, 16), device="cuda"), Y, Wt, P, dY, dWt)
+    assert dWt.tolist() == [[0.0, 48.0], [0.0, 0.0]] and bool((dY[2] == 2.0).all()) and not bool(dY[[0, 1, 3]].any())
+
+
+# ---- as a whole ---------------------------------------------------------------------------------------------------------------
+
+
+def _layer(dtype, T, E, k, D, H, seed):
+    """(calls, outputs): a table, a router, two products and the sum, forward and gradients, all buffers made beforehand."""
+    e = lambda *s, t=dtype: torch.full(s, float("nan"), dtype=t, device="cuda")  # noqa: E731
+    i = lambda *s: torch.full(s, 77, dtype=torch.int32, device="cuda")  # noqa: E731
+    V, R = 50, T * k
+    LUT, Idx = _rand((V, D), dtype, seed), _ints(np.random.default_rng(seed).integers(0, V, T))
+    W1, W2, L = _rand((E, H, D), dtype, seed + 1, D ** -0.5), _rand((E, D, H), dtype, seed + 2, H ** -0.5), _rand((T, E), dtype, seed + 3)
+    dO = _rand((T, D), dtype, seed + 4)
+    X, Wt, Id, Off, Row, Place = e(T, D), e(T, k, t=torch.float32), i(T, k), i(E + 1), i(R), i(T, k)
+    A, Y, O = e(R, H), e(R, D), e(T, D)
+    dY, dWt, dA, dXr, dX, dL = torch.zeros((R, D), dtype=dtype, device="cuda"), e(T, k, t=torch.float32), e(R, H), e(R, D), e(T, D), e(T, E)
+    dW1, dW2, dLUT = e(E, H, D, t=torch.float32), e(E, D, H), e(V, D, t=torch.float32)
+    ws = [_bytes(max(1, n)) for n in (tc.tc_route_workspace_bytes(T, E, k), tc.tc_embed_grad_workspace_bytes(V, D, T), tc.tc_expert_mm_grad_w_workspace_bytes(R, E, H, D),
+                                      tc.tc_expert_mm_grad_w_workspace_bytes(R, E, D, H))]
+
+    def calls(stream=None):
+        s = dict(stream=stream)
+        tc.tc_embed(LUT, Idx, X, 2.0, **s)
+        tc.tc_route(L, Wt, Id, Off, Row, Place, ws[0], True, **s)
+        tc.tc_expert_mm(X, W1, Off, Row, A, True, **s)
+        tc.tc_expert_mm(A, W2, Off, None, Y, **s)
+        tc.tc_expert_sum(Y, Wt, Place, O, **s)
+        tc.tc_expert_sum_grad(dO, Y, Wt, Place, dY, dWt, **s)
+        tc.tc_route_grad(L, Id, dWt, dL, True, **s)
+        tc.tc_expert_mm_grad_w(dY, A, Off, None, dW2, ws[3], **s)
+        tc.tc_expert_mm_grad_x(dY, W2, Off, A, dA, **s)
+        tc.tc_expert_mm_grad_w(dA, X, Off, Row, dW1, ws[2], **s)
+        tc.tc_expert_mm_grad_x(dA, W1, Off, None, dXr, **s)
+        tc.tc_expert_sum(dXr, None, Place, dX, **s)
+        tc.tc_embed_grad(dX, Idx, dLUT, ws[1], 2.0, **s)
+
+    return calls, dict(X=X, Wt=Wt, Id=Id, Off=Off, Row=Row, Place=Place, A=A, Y=Y, O=O, dY=dY, dWt=dWt, dL=dL, dW2=dW2, dA=dA, dW1=dW1, dXr=dXr, dX=dX, dLUT=dLUT), \
+        dict(LUT=LUT, Idx=Idx, W1=W1, W2=W2, L=L, dO=dO)
+
+
+@pytest.mark.parametrize("T,D,H", [(3, 16, 24), (200, 72, 130)])
+def test_a_layer_by_differences(T, D, H):
+    """The gradients of a whole layer in float32 against central differences of the layer in 64 bits, along random directions."""
+    E, k, h = 4, 2, 1e-5
+    calls, out, par = _layer(torch.float32, T, E, k, D, H, 20)
+    calls()
+    p = {n: _np(v) for n, v in par.items()}
+    ids = _np(out["Id"])
+
+    def loss(q):
+        X = 2.0 * q["LUT"][p["Idx"]]
+        w = ref.softmax_rows(np.take_along_axis(q["L"], ids, 1))
+        O = np.zeros_like(p["dO"])
+        for t, i in np.ndindex(*ids.shape):
+            O[t] += w[t, i] * (q["W2"][ids[t, i]] @ np.maximum(q["W1"][ids[t, i]] @ X[t], 0.0))
+        return (O * p["dO"]).sum()
+
+    rng = np.random.default_rng(21)
+    for name, grad in (("LUT", "dLUT"), ("W1", "dW1"), ("W2", "dW2"), ("L", "dL")):
+        g = _np(out[grad])
+        v = rng.standard_normal(g.shape)
+        v /= np.linalg.norm(v)
+        up, down = dict(p), dict(p)
+        up[name], down[name] = p[name] + h * v, p[name] - h * v
+        # float32 stages: 1e-4 of the gradient's norm; a unit whose input crosses 0 within h: a few parts in 1e4 more
+        assert abs((loss(up) - loss(down)) / (2 * h) - (g * v).sum()) < 1e-3 * np.linalg.norm(g) + 1e-6, name
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_a_layer_in_a_graph_and_on_another_stream(dtype):
+    for T in (5, 150):
+        calls, out, _ = _layer(dtype, T, 5, 2, 40, 72, 30)
+        calls()
+        torch.cuda.synchronize()
+        want = {n: v.clone() for n, v in out.items()}
+        assert not any(bool(v.isnan().any()) for v in want.values() if v.is_floating_point())
+
+        def spoil():
+            for n, v in out.items():
+                v.fill_(float("nan") if v.is_floating_point() and n != "dY" else 0)
+
+        spoil()
+        torch.cuda.synchronize()
+        other = torch.cuda.Stream()
+        calls(other.cuda_stream)
+        other.synchronize()
+        assert all(torch.equal(out[n], want[n]) for n in want)
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            calls()
+        for _ in range(3):
+            spoil()
+            g.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(out[n], want[n]) for n in want)
+
+
+# ---- refusals -------------------------------------------------------------------------------------------------------------------
+
+
+def test_refusals_of_the_binding():
+    f = lambda *s, t=torch.float32: torch.zeros(s, dtype=t, device="cuda")  # noqa: E731
+    i = lambda *s: torch.zeros(s, dtype=torch.int32, device="cuda")  # noqa: E731
+    with pytest.raises(TypeError):
+        tc.tc_embed(f(4, 8, t=torch.float64), i(2), f(2, 8))
+    with pytest.raises(TypeError):
+        tc.tc_embed(f(4, 8), i(2), f(2, 8, t=torch.bfloat16))
+    with pytest.raises(TypeError):
+        tc.tc_embed(f(4, 8), i(2).long(), f(2, 8))
+    with pytest.raises(TypeError):
+        tc.tc_embed(f(4, 8).cpu(), i(2), f(2, 8))
+    with pytest.raises(ValueError):
+        tc.tc_embed(f(8, 4).t(), i(2), f(2, 8))
+    with pytest.raises(ValueError):
+        tc.tc_embed(f(4, 8), i(3), f(2, 8))
+    with pytest.raises(tc.TcError):
+        tc.tc_embed(f(4, 8), i(2), f(17)[1:].view(2, 8))  # not 16-byte aligned
+    with pytest.raises(tc.TcError):
+        tc.tc_embed_grad(f(2, 8), i(2), f(4, 8), None)  # no workspace
+    with pytest.raises(TypeError):
+        tc.tc_embed_grad(f(2, 8), i(2), f(4, 8, t=torch.bfloat16), f(4096))
+    with pytest.raises(tc.TcError):
+        tc.tc_route(f(70, 4), f(70, 2), i(70, 2), i(5), i(140), i(70, 2))  # no workspace
+    with pytest.raises(tc.TcError):
+        tc.tc_route(f(1, 2000), f(1, 2), i(1, 2), i(2001), i(2), i(1, 2))  # more experts than it takes
+    with pytest.raises(ValueError):
+        tc.tc_route(f(3, 4), f(3, 2), i(3, 2), i(4), i(6), i(3, 2))
+    with pytest.raises(ValueError):
+        tc.tc_expert_mm(f(3, 8), f(2, 4, 9), i(3), None, f(3, 4))
+    with pytest.raises(ValueError):
+        tc.tc_expert_mm(f(4, 8), f(2, 4, 8), i(3), None, f(3, 4))
+    with pytest.raises(TypeError):
+        tc.tc_expert_mm(f(3, 8), f(2, 4, 8, t=torch.float16), i(3), None, f(3, 4))
+    x = f(4, 4)
+    with pytest.raises(tc.TcError):
+        tc.tc_expert_mm(x, f(2, 4, 4), i(3), None, x)  # the output is an input
+    with pytest.raises(ValueError):
+        tc.tc_expert_mm_grad_x(f(3, 4), f(2, 4, 8), i(3), f(3, 7), f(3, 8))
+    with pytest.raises(TypeError):
+        tc.tc_expert_mm_grad_w(f(3, 4), f(3, 8), i(3), None, f(2, 4, 8, t=torch.float16))
+    with pytest.raises(ValueError):
+        tc.tc_expert_sum(f(6, 8), f(3, 2), i(3, 3), f(3, 8))
+    with pytest.raises(ValueError):
+        tc.tc_expert_sum_grad(f(3, 8), f(6, 8), f(3, 2), i(3, 2), f(5, 8), f(3, 2))
