@@ -109,7 +109,8 @@ int64_t tc355_get_option(tc_option key);
  *   embed, expert_sum, expert_sum_grad, route_grad: rows
  *   embed_grad: small_sort, sort
  *   route:  one, tiles
- *   expert_mm, expert_mm_grad_x, expert_mm_grad_w: tile
+ *   expert_mm: rows (experts with few rows), tile
+ *   expert_mm_grad_x, expert_mm_grad_w: tile
  * A debugging and testing aid: tests pick the tolerance of the
  * arithmetic that actually ran instead of re-deriving the dispatch.
  */
@@ -414,8 +415,8 @@ tc_status tc_lut(int32_t n_tables, const float *const *LUT,
  *    the router are fp32, indices int32.
  *  - Every result is the same each time: no sum depends on the order in which
  *    workgroups run.
- *  - Extents below 2^30 unless said otherwise (rows of the table: below
- *    2^31 - 1); tensors may hold more than 2^31 elements.
+ *  - Extents below 2^30 (rows of a table: below 2^31 - 1; N and K of the
+ *    products: below 2^22); tensors may hold more than 2^31 elements.
  *  - A pointer to an array without elements may be NULL.
  *  - Indices and offsets live on the device, so the host cannot reject them.  Whatever they hold, nothing
  *    outside the named arrays is read or written.

@@ -5,16 +5,16 @@
 // What bounds them: 2 R N K operations each on the matrix core, unless an expert has so few rows that its weights' bytes do
 // (expert_rows.hpp takes those).
 //
-// A workgroup computes a BM x BN tile of one expert.  In a stage both operands' next 128 bytes of the reduction (64 elements of 16
-// bits, 32 of 32) go straight from memory to LDS, 16 bytes per lane, while the stage before is multiplied: two buffers, one
-// barrier a stage.  The fragments of a stage are all read before the next stage's loads are issued: the compiler, which knows of
-// the loads to LDS, would wait for them before any LDS read that follows.
+// A workgroup computes a BM x BN tile of one expert, a stage of 128 bytes of the reduction (64 elements of 16 bits, 32 of 32) at a time:
+// whole cache lines of an operand's rows, whose loads take the address path half the time of half lines.  Stages go straight from
+// memory to a ring of D buffers in LDS, 16 bytes per lane, D - 1 stages ahead.  A stage is multiplied in two halves; the fragments of the
+// next half are read meanwhile, so that the matrix core waits for nothing but the one barrier a stage.
 //
 // Layout in LDS.  Along its rows an operand is [rows][128 bytes]; the 16-byte chunk c of row r lies in slot c ^ (r & 7), so that
 // the 16 rows of a fragment read hit all banks.  Across its rows it is [reduction][tile columns]: 16-bit elements are
 // read by the transposing LDS read (four rows of 16 columns to 16 lanes of four), 32-bit ones word by word; chunks are swizzled by
 // the rows that one instruction reads together.  Lane (i = lane % 16, q = lane / 16) of a matrix instruction supplies row i and, of the
-// reduction, elements 8q .. 8q+7 of 32 (16 bits) or, in 4 instructions, 4q .. 4q+3 of 16 (32 bits): the order is free as long as
+// half stage, elements 8q .. 8q+7 of 32 (16 bits) or, in 4 instructions, 4q .. 4q+3 of 16 (32 bits): the order is free as long as
 // both operands keep it.  The operands are exchanged (weights first), so that a lane's four results are neighbours in a row of the output.
 //
 // Sums are fp32 in the matrix core's accumulators whatever the storage, and each output is rounded once.
@@ -31,12 +31,9 @@ template <int N>
 __device__ __forceinline__ void emm_wait() {
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
-__device__ __forceinline__ void emm_to_lds(const char* g, unsigned lds) {  // lane l's 16 bytes to lds + 16 l (a uniform address)
-  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(uintptr_t)g,
-                                   (__attribute__((address_space(3))) void*)(uintptr_t)lds, 16, 0, 0);
-}
-__device__ __forceinline__ unsigned lds_address(const void* p) {
-  return (unsigned)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
+typedef __attribute__((address_space(3))) char lds_char;
+__device__ __forceinline__ void emm_to_lds(const char* g, lds_char* lds) {  // lane l's 16 bytes to lds + 16 l (a uniform address)
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(uintptr_t)g, (__attribute__((address_space(3))) void*)lds, 16, 0, 0);
 }
 
 // ---- which rows a tile takes ------------------------------------------------------------------------------------------
@@ -47,39 +44,39 @@ struct ExpertTile {
   int m, n;    // tile of the expert, in rows and columns
 };
 
-// Tile `at` of all, or false.  Off is the device's: whatever it holds, rows stay inside [0, R).  Tiles of one expert follow each
+// Workgroup `bid`'s tile, or false.  Off is the device's: whatever it holds, rows stay inside [0, R).  Tiles of one expert follow each
 // other in blocks of 8 row tiles by all column tiles, row tiles first, so that workgroups that run together share operands; and every
-// XCD (workgroups equal modulo 8) takes a run of its own.
+// XCD (workgroups equal modulo 8) takes a run of its own.  One round trip to memory for up to 63 experts.
 __device__ __forceinline__ bool expert_tile(const int* off, int E, int R, int bm, int nt, unsigned bid, ExpertTile* t) {
   const int lane = threadIdx.x & 63;
-  unsigned total = 0;
-  for (int base = 0; base <= E; base += 64) {
-    const int g = base + lane;
-    int c = 0;
-    if (g <= E) c = (g < E ? min(max(off[g + 1], 0), R) : R) - min(max(off[g], 0), R);
-    unsigned n = c > 0 ? (unsigned)((c + bm - 1) / bm) * nt : 0;
+  int lo, hi;
+  const auto tiles = [&](int g) {  // of expert g; its rows go to lo, hi
+    lo = hi = 0;
+    if (g <= E) {
+      lo = min(max(off[g], 0), R);
+      hi = g < E ? min(max(off[g + 1], 0), R) : R;
+    }
+    return hi > lo ? (unsigned)((hi - lo + bm - 1) / bm) * nt : 0u;
+  };
+  const auto up_to = [&](unsigned n) {  // inclusive sums over the lanes
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) n += __shfl_xor(n, d);
-    total += n;
-  }
+    for (int d = 1; d < 64; d *= 2) {
+      const unsigned o = __shfl_up(n, d);
+      if (lane >= d) n += o;
+    }
+    return n;
+  };
+  unsigned n = tiles(lane), incl = up_to(n), total = __shfl(incl, 63);
+  for (int base = 64; base <= E; base += 64) total += __shfl(up_to(tiles(base + lane)), 63);
   const unsigned run = (total + 7) / 8;
   if (bid / 8 >= run) return false;
   const unsigned at = (bid & 7) * run + bid / 8;
   if (at >= total) return false;
   unsigned before = 0;
   for (int base = 0; base <= E; base += 64) {
-    const int g = base + lane;
-    int lo = 0, hi = 0;
-    if (g <= E) {
-      lo = min(max(off[g], 0), R);
-      hi = g < E ? min(max(off[g + 1], 0), R) : R;
-    }
-    const unsigned n = hi > lo ? (unsigned)((hi - lo + bm - 1) / bm) * nt : 0;
-    unsigned incl = n;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      const unsigned o = __shfl_up(incl, d);
-      if (lane >= d) incl += o;
+    if (E >= 64) {
+      n = tiles(base + lane);
+      incl = up_to(n);
     }
     const unsigned long long past = __ballot(at < before + incl);
     if (past) {
@@ -117,163 +114,187 @@ __device__ __forceinline__ u4 emm_load_any(const T* p, int left) {
 }
 
 // Operand along its rows: ROWS rows of the tile, 128 bytes of the reduction a stage.  NW wavefronts load it, 8 rows an instruction.
-template <typename T, int ROWS, int NW>
+// ANYWHERE: the rows lie anywhere (an address per lane and instruction); else within 4 GB of each other, from a base that all share.
+template <typename T, int ROWS, int NW, bool ANYWHERE>
 struct AlongRows {
+  static constexpr bool ACROSS = false;
   static constexpr int BYTES = ROWS * EMM_STAGE;
   static constexpr int PER = ROWS / 8 / NW;  // instructions of a wavefront
   static constexpr int BK = EMM_STAGE / sizeof(T);
   static_assert(PER * 8 * NW == ROWS, "whole instructions");
-  const T* p[PER];  // this lane's row, at its chunk of the first stage; nullptr: a row of zeros
-  int at;           // element of the reduction where the chunk begins
-  int Q;
+  const char* p[ANYWHERE ? PER : 1];  // this lane's rows at its chunk of the stage, or the base there
+  unsigned off[ANYWHERE ? 1 : PER];
+  int at, q0, Q;  // the chunk's first element in a stage; the stage's first one; all
   u4 held[PER];
 
-  // row(j): the source row of row j of the tile, or -1
+  // row(j): where row j of the tile lies among those of `b`
   template <typename F>
-  __device__ __forceinline__ void begin(const T* base, int64_t ld, int q, int wave, int lane, F row) {
+  __device__ __forceinline__ void begin(const T* b, int64_t ld, int q, int wave, int lane, F row) {
     Q = q;
+    q0 = 0;
     at = ((lane & 7) ^ (lane >> 3)) * Elem<T>::PER16;  // (row & 7 = lane / 8)
+    if constexpr (!ANYWHERE) p[0] = reinterpret_cast<const char*>(b);
 #pragma unroll
     for (int j = 0; j < PER; j++) {
       const int64_t r = row((wave * PER + j) * 8 + (lane >> 3));
-      p[j] = r < 0 ? nullptr : base + r * ld + at;
+      if constexpr (ANYWHERE) p[j] = reinterpret_cast<const char*>(b + r * ld + at);
+      else off[j] = (unsigned)(r * ld + at) * (unsigned)sizeof(T);
     }
   }
-  __device__ __forceinline__ void to_lds(unsigned lds, int wave) {
-    const bool in = at < Q;
+  __device__ __forceinline__ const char* where(int j) const {
+    if constexpr (ANYWHERE) return p[j];
+    else return p[0] + off[j];
+  }
+  __device__ __forceinline__ void to_lds(lds_char* lds, int wave, int) {
+    if (q0 + BK <= Q) {
 #pragma unroll
-    for (int j = 0; j < PER; j++) {
-      const char* src = in && p[j] ? reinterpret_cast<const char*>(p[j]) : reinterpret_cast<const char*>(emm_zeros);
-      emm_to_lds(src, lds + (wave * PER + j) * 1024);
+      for (int j = 0; j < PER; j++) emm_to_lds(where(j), lds + (wave * PER + j) * 1024);
+    } else {
+      const bool in = q0 + at < Q;
+#pragma unroll
+      for (int j = 0; j < PER; j++) emm_to_lds(in ? where(j) : reinterpret_cast<const char*>(emm_zeros), lds + (wave * PER + j) * 1024);
     }
     next();
   }
-  __device__ __forceinline__ void hold() {
+  __device__ __forceinline__ void hold(int, int) {
 #pragma unroll
     for (int j = 0; j < PER; j++) {
       held[j] = u4{0, 0, 0, 0};
-      if (p[j] && at < Q) held[j] = emm_load_any(p[j], Q - at);
+      if (q0 + at < Q) held[j] = emm_load_any(reinterpret_cast<const T*>(where(j)), Q - q0 - at);
     }
     next();
   }
-  __device__ __forceinline__ void put(char* lds, int wave, int lane) {
+  __device__ __forceinline__ void put(lds_char* lds, int wave, int lane) {
 #pragma unroll
-    for (int j = 0; j < PER; j++) *reinterpret_cast<u4*>(lds + (wave * PER + j) * 1024 + lane * 16) = held[j];
+    for (int j = 0; j < PER; j++) *(__attribute__((address_space(3))) u4*)(lds + (wave * PER + j) * 1024 + lane * 16) = held[j];
   }
   __device__ __forceinline__ void next() {
-    at += BK;
+    q0 += BK;
 #pragma unroll
-    for (int j = 0; j < PER; j++) p[j] = p[j] ? p[j] + BK : nullptr;
+    for (int j = 0; j < (ANYWHERE ? PER : 1); j++) p[j] += EMM_STAGE;
   }
-  // 16 bytes of row r of the tile, chunk 4 s + q
-  static __device__ __forceinline__ const char* chunk(const char* lds, int r, int s, int q) {
-    return lds + r * EMM_STAGE + (((4 * s + q) ^ (r & 7)) * 16);
+  // rows r0 .. r0+15 of the tile, half s of the stage: 16 bytes of row r0 + i, chunk 4 s + q
+  static __device__ __forceinline__ u4 fragment(const lds_char* lds, int r0, int s, int i, int q) {
+    return *(const __attribute__((address_space(3))) u4*)(lds + (r0 + i) * EMM_STAGE + (((4 * s + q) ^ (i & 7)) * 16));
   }
 };
 
 // Operand across its rows: BK rows of the reduction a stage, COLS columns of the tile.
-template <typename T, int COLS, int NW>
+// ANYWHERE: the reduction goes through rows that a list names; else through neighbours.
+template <typename T, int COLS, int NW, bool ANYWHERE>
 struct AcrossRows {
+  static constexpr bool ACROSS = true;
   static constexpr int BK = EMM_STAGE / sizeof(T);
   static constexpr int BYTES = BK * COLS * sizeof(T);
   static constexpr int CPR = COLS * sizeof(T) / 16;  // chunks of a row
   static constexpr int RPI = 64 / CPR;               // rows of an instruction
   static constexpr int PER = BK / RPI / NW;
   static_assert(RPI * CPR == 64 && PER * RPI * NW == BK, "whole instructions");
-  const T* base;  // column 0 of the reduction's row 0
-  const int* row; // rows of `base` that the reduction goes through, or nullptr: all of them in order
+  const T* base;    // the stage's first row; ANYWHERE: row 0
+  const int* row;   // ANYWHERE: rows of `base` that the reduction goes through, from the next but one stage on
   int64_t ld;
-  int q0, Q, rows;  // row of the reduction that the next stage begins with; their number; rows of `base`
-  int left[PER];    // (any alignment) elements of the row from the chunk on
-  int col[PER];
-  int src[PER];
+  int q0, Q, rows;  // the stage's first row of the reduction, their number; rows of `base`
+  int cols;
+  int col[PER];     // first column of the chunk; beyond the last column any chunk will do
+  unsigned off[ANYWHERE ? 1 : PER];
+  int src[ANYWHERE ? PER : 1];
   u4 held[PER];
 
   // rows that one instruction reads together have different chunks of 64 banks
   static __device__ __forceinline__ int swizzle(int r) {
-    if constexpr (sizeof(T) == 2) return 2 * ((r & 3) | ((r >> 1) & 4));
-    else return 4 * ((r >> 2) & 3);
+    if constexpr (sizeof(T) == 4) return 4 * ((r >> 2) & 3);
+    else if constexpr (CPR >= 16) return 2 * ((r & 3) | ((r >> 1) & 4));
+    else return 2 * (((r >> 1) & 1) | ((r >> 2) & 2));  // (a row is half the banks: neighbouring rows differ anyway)
   }
-  __device__ __forceinline__ int at(int j, int wave, int lane) const { return (wave * PER + j) * RPI + lane / CPR; }
+  static __device__ __forceinline__ int at(int j, int wave, int lane) { return (wave * PER + j) * RPI + lane / CPR; }
 
-  __device__ __forceinline__ void begin(const T* b, int64_t stride, const int* rw, int q, int total, int c0, int cols, int wave, int lane) {
+  template <bool ANY>
+  __device__ __forceinline__ void begin(const T* b, int64_t stride, const int* rw, int q, int total, int c0, int width, int wave, int lane) {
     base = b;
     row = rw;
     ld = stride;
     q0 = 0;
     Q = q;
     rows = total;
+    cols = width;
 #pragma unroll
     for (int j = 0; j < PER; j++) {
       col[j] = c0 + ((lane % CPR) ^ swizzle(at(j, wave, lane))) * Elem<T>::PER16;
-      left[j] = cols - col[j];
+      if (!ANY) col[j] = min(col[j], cols - Elem<T>::PER16);
+      if constexpr (!ANYWHERE) off[j] = (unsigned)(at(j, wave, lane) * ld + col[j]) * (unsigned)sizeof(T);
     }
-    look(wave, lane);
+    if constexpr (ANYWHERE) look(wave, lane);
   }
-  // the source rows of the stage at q0, -1: zeros
+  // the source rows of the stage at q0; -1: zeros
   __device__ __forceinline__ void look(int wave, int lane) {
 #pragma unroll
     for (int j = 0; j < PER; j++) {
       const int q = q0 + at(j, wave, lane);
       src[j] = -1;
-      if (q < Q) src[j] = row ? row[q] : q;
+      if (q < Q) src[j] = row[q];
     }
   }
-  __device__ __forceinline__ bool there(int j) const { return src[j] >= 0 && src[j] < rows && left[j] > 0; }
-  __device__ __forceinline__ void to_lds(unsigned lds, int wave, int lane) {
+  __device__ __forceinline__ const T* where(int j) const {
+    if constexpr (ANYWHERE) return base + (int64_t)src[j] * ld + col[j];
+    else return reinterpret_cast<const T*>(reinterpret_cast<const char*>(base) + off[j]);
+  }
+  __device__ __forceinline__ bool there(int j, int wave, int lane) const {
+    if constexpr (ANYWHERE) return src[j] >= 0 && src[j] < rows;
+    else return q0 + at(j, wave, lane) < Q;
+  }
+  __device__ __forceinline__ void to_lds(lds_char* lds, int wave, int lane) {
+    if (!ANYWHERE && q0 + BK <= Q) {
 #pragma unroll
-    for (int j = 0; j < PER; j++) {
-      const char* s = there(j) ? reinterpret_cast<const char*>(base + (int64_t)src[j] * ld + col[j]) : reinterpret_cast<const char*>(emm_zeros);
-      emm_to_lds(s, lds + (wave * PER + j) * 1024);
+      for (int j = 0; j < PER; j++) emm_to_lds(reinterpret_cast<const char*>(where(j)), lds + (wave * PER + j) * 1024);
+    } else {
+#pragma unroll
+      for (int j = 0; j < PER; j++) {
+        const char* s = there(j, wave, lane) ? reinterpret_cast<const char*>(where(j)) : reinterpret_cast<const char*>(emm_zeros);
+        emm_to_lds(s, lds + (wave * PER + j) * 1024);
+      }
     }
-    q0 += BK;
-    look(wave, lane);
+    next(wave, lane);
   }
   __device__ __forceinline__ void hold(int wave, int lane) {
 #pragma unroll
     for (int j = 0; j < PER; j++) {
       held[j] = u4{0, 0, 0, 0};
-      if (there(j)) held[j] = emm_load_any(base + (int64_t)src[j] * ld + col[j], left[j]);
+      if (col[j] < cols && there(j, wave, lane)) held[j] = emm_load_any(where(j), cols - col[j]);
     }
-    q0 += BK;
-    look(wave, lane);
+    next(wave, lane);
   }
-  __device__ __forceinline__ void put(char* lds, int wave, int lane) {
+  __device__ __forceinline__ void put(lds_char* lds, int wave, int lane) {
 #pragma unroll
-    for (int j = 0; j < PER; j++) *reinterpret_cast<u4*>(lds + (wave * PER + j) * 1024 + lane * 16) = held[j];
+    for (int j = 0; j < PER; j++) *(__attribute__((address_space(3))) u4*)(lds + (wave * PER + j) * 1024 + lane * 16) = held[j];
   }
-  // 16 bits: rows 32 s + 8 q + 4 h + (0..3), columns c .. c+15: this lane's address of the transposing read
-  static __device__ __forceinline__ unsigned four(unsigned lds, int c, int s, int h, int i, int q) {
-    const int r = 32 * s + 8 * q + 4 * h + (i >> 2), cc = c + (i & 3) * 4;
-    return lds + r * (COLS * 2) + (((cc >> 3) ^ swizzle(r)) * 16) + (cc & 7) * 2;
+  __device__ __forceinline__ void next(int wave, int lane) {
+    q0 += BK;
+    if constexpr (ANYWHERE) look(wave, lane);
+    else base += BK * ld;
   }
-  // 32 bits: row 16 s + 4 q + e, column c
-  static __device__ __forceinline__ float word(const char* lds, int c, int s, int e, int q) {
-    const int r = 16 * s + 4 * q + e;
-    return *reinterpret_cast<const float*>(lds + r * (COLS * 4) + (((c >> 2) ^ swizzle(r)) * 16) + (c & 3) * 4);
+  // columns c0 .. c0+15 of the tile, half s of the stage, the reduction's elements as along rows
+  static __device__ __forceinline__ u4 fragment(const lds_char* lds, int c0, int s, int i, int q) {
+    if constexpr (sizeof(T) == 2) {
+      // rows 32 s + 8 q + 4 h + (0..3): this lane's address of the transposing read is that of 4 elements of one row
+      s4v v[2];
+#pragma unroll
+      for (int h = 0; h < 2; h++) {
+        const int r = 32 * s + 8 * q + 4 * h + (i >> 2), c = c0 + (i & 3) * 4;
+        v[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4v*)(const_cast<lds_char*>(lds) + r * (COLS * 2) +
+                                                                                              (((c >> 3) ^ swizzle(r)) * 16) + (c & 7) * 2));
+      }
+      return __builtin_bit_cast(u4, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7));
+    } else {
+      f4 v;
+#pragma unroll
+      for (int e = 0; e < 4; e++) {
+        const int r = 16 * s + 4 * q + e, c = c0 + i;
+        v[e] = *(const __attribute__((address_space(3))) float*)(lds + r * (COLS * 4) + (((c >> 2) ^ swizzle(r)) * 16) + (c & 3) * 4);
+      }
+      return __builtin_bit_cast(u4, v);
+    }
   }
 };
-
-// A fragment: 16 rows (or columns) of the tile by 64 bytes of the reduction, 16 bytes a lane.
-template <typename T, int ROWS, int NW>
-__device__ __forceinline__ u4 emm_fragment(const AlongRows<T, ROWS, NW>&, const char* lds, int r0, int s, int i, int q) {
-  return *reinterpret_cast<const u4*>(AlongRows<T, ROWS, NW>::chunk(lds, r0 + i, s, q));
-}
-template <typename T, int COLS, int NW>
-__device__ __forceinline__ u4 emm_fragment(const AcrossRows<T, COLS, NW>&, const char* lds, int c0, int s, int i, int q) {
-  if constexpr (sizeof(T) == 2) {
-    typedef __attribute__((address_space(3))) s4v* at;
-    const unsigned base = lds_address(lds);
-    const s4v a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((at)(uintptr_t)AcrossRows<T, COLS, NW>::four(base, c0, s, 0, i, q));
-    const s4v b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((at)(uintptr_t)AcrossRows<T, COLS, NW>::four(base, c0, s, 1, i, q));
-    return __builtin_bit_cast(u4, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
-  } else {
-    f4 v;
-#pragma unroll
-    for (int e = 0; e < 4; e++) v[e] = AcrossRows<T, COLS, NW>::word(lds, c0 + i, s, e, q);
-    return __builtin_bit_cast(u4, v);
-  }
-}
 
 template <typename T>
 __device__ __forceinline__ f4 emm_mfma(u4 a, u4 b, f4 c) {
@@ -291,88 +312,96 @@ __device__ __forceinline__ f4 emm_mfma(u4 a, u4 b, f4 c) {
 
 // ---- the loop over the reduction ----------------------------------------------------------------------------------------
 
-// MI x NI blocks of 16 x 16 per wavefront, at row rm and column cn of the tile.
-template <typename T, bool ANY, int MI, int NI, typename A, typename B>
-__device__ __forceinline__ void emm_stage(const A& a, const B& b, const char* la, const char* lb, int rm, int cn, int i, int q, u4 (&fa)[2][MI], u4 (&fb)[2][NI]) {
+// Traffic of half a stage: what goes into buffer `then`, and the fragments of half s that come out of buffer `now`.  (Restricted
+// pointers of a function of their own: the compiler would wait for all loads to LDS before any LDS read that they might concern.)
+template <bool ANY, int MI, int NI, typename A, typename B>
+__device__ __forceinline__ void emm_traffic(A& a, B& b, const lds_char* __restrict__ now, lds_char* __restrict__ then, int s, bool read, bool more, bool held,
+                                            int rm, int cn, int wave, int lane, u4 (&fa)[MI], u4 (&fb)[NI]) {
+  const int i = lane & 15, q = lane >> 4;
+  if constexpr (ANY) {
+    if (held) {
+      a.put(then, wave, lane);
+      b.put(then + A::BYTES, wave, lane);
+    }
+    if (more) {
+      a.hold(wave, lane);
+      b.hold(wave, lane);
+    }
+  } else {
+    if (more) {
+      a.to_lds(then, wave, lane);
+      b.to_lds(then + A::BYTES, wave, lane);
+    }
+  }
+  if (read) {
 #pragma unroll
-  for (int s = 0; s < 2; s++) {
+    for (int n = 0; n < NI; n++) fb[n] = B::fragment(now + A::BYTES, cn + 16 * n, s, i, q);
 #pragma unroll
-    for (int m = 0; m < MI; m++) fa[s][m] = emm_fragment(a, la, rm + 16 * m, s, i, q);
-#pragma unroll
-    for (int n = 0; n < NI; n++) fb[s][n] = emm_fragment(b, lb, cn + 16 * n, s, i, q);
+    for (int m = 0; m < MI; m++) fa[m] = A::fragment(now, rm + 16 * m, s, i, q);
   }
 }
 
-template <typename A>
-struct EmmIsAcross {
-  static constexpr bool value = false;
-};
-template <typename T, int C, int NW>
-struct EmmIsAcross<AcrossRows<T, C, NW>> {
-  static constexpr bool value = true;
-};
-
-template <typename A>
-__device__ __forceinline__ void emm_to_lds(A& a, unsigned lds, int wave, int lane) {
-  if constexpr (EmmIsAcross<A>::value) a.to_lds(lds, wave, lane);
-  else a.to_lds(lds, wave);
-}
-template <typename A>
-__device__ __forceinline__ void emm_hold(A& a, int wave, int lane) {
-  if constexpr (EmmIsAcross<A>::value) a.hold(wave, lane);
-  else a.hold();
+// Until at most `stages` stages' loads (P a stage) are in flight.
+template <int P, int MOST>
+__device__ __forceinline__ void emm_wait_stages(int stages) {
+  if constexpr (MOST > 0) {
+    if (stages < MOST) return emm_wait_stages<P, MOST - 1>(stages);
+  }
+  emm_wait<P * MOST>();
 }
 
-template <typename T, bool ANY, int MI, int NI, typename A, typename B>
-__device__ __forceinline__ void emm_loop(A& a, B& b, char* lds, int stages, int rm, int cn, int wave, int lane, f4 (&acc)[MI][NI]) {
-  constexpr int STAGE = A::BYTES + B::BYTES;
-  const int i = lane & 15, q = lane >> 4;
-  const unsigned base = lds_address(lds);
+// MI x NI blocks of 16 x 16 per wavefront, at row rm and column cn of the tile.
+template <typename T, bool ANY, int D, int MI, int NI, typename A, typename B>
+__device__ __forceinline__ void emm_loop(A& a, B& b, lds_char* lds, int stages, int rm, int cn, int wave, int lane, f4 (&acc)[MI][NI]) {
+  constexpr int STAGE = A::BYTES + B::BYTES, P = A::PER + B::PER;
 #pragma unroll
   for (int m = 0; m < MI; m++)
 #pragma unroll
     for (int n = 0; n < NI; n++) acc[m][n] = f4{0, 0, 0, 0};
   if (stages <= 0) return;
-  if constexpr (ANY) {
-    emm_hold(a, wave, lane);
-    emm_hold(b, wave, lane);
-    a.put(lds, wave, lane);
-    b.put(lds + A::BYTES, wave, lane);
+  u4 fa[2][MI], fb[2][NI];
+  if constexpr (ANY) {  // stage t + 2 is written, and t + 3 fetched, while the second half of stage t is multiplied
+    static_assert(D == 2, "buffers");
+#pragma unroll
+    for (int j = 0; j < 2; j++) {
+      a.hold(wave, lane);
+      b.hold(wave, lane);
+      a.put(lds + j * STAGE, wave, lane);
+      b.put(lds + j * STAGE + A::BYTES, wave, lane);
+    }
+    a.hold(wave, lane);
+    b.hold(wave, lane);
   } else {
-    emm_to_lds(a, base, wave, lane);
-    emm_to_lds(b, base + A::BYTES, wave, lane);
+#pragma unroll
+    for (int j = 0; j < D; j++)
+      if (j < stages) {
+        a.to_lds(lds + j * STAGE, wave, lane);
+        b.to_lds(lds + j * STAGE + A::BYTES, wave, lane);
+      }
+    emm_wait_stages<P, D - 1>(stages - 1);
   }
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+  emm_traffic<ANY, MI, NI>(a, b, lds, lds, 0, true, false, false, rm, cn, wave, lane, fa[0], fb[0]);
+  int at = 0;  // buffer of stage t
   for (int t = 0; t < stages; t++) {
-    char* now = lds + (t & 1) * STAGE;
-    emm_wait<0>();
-    __syncthreads();  // this stage is in LDS, and everyone has read the one before
-    u4 fa[2][MI], fb[2][NI];
-    emm_stage<T, ANY, MI, NI>(a, b, now, now + A::BYTES, rm, cn, i, q, fa, fb);
-    __builtin_amdgcn_sched_barrier(0);
-    if (t + 1 < stages) {
-      if constexpr (ANY) {
-        emm_hold(a, wave, lane);
-        emm_hold(b, wave, lane);
-      } else {
-        const unsigned then = base + ((t + 1) & 1) * STAGE;
-        emm_to_lds(a, then, wave, lane);
-        emm_to_lds(b, then + A::BYTES, wave, lane);
-      }
-    }
-    __builtin_amdgcn_sched_barrier(0);
+    lds_char* const now = lds + at * STAGE;
+    at = at + 1 == D ? 0 : at + 1;
+    emm_traffic<ANY, MI, NI>(a, b, now, now, 1, true, false, false, rm, cn, wave, lane, fa[1], fb[1]);
 #pragma unroll
-    for (int s = 0; s < 2; s++)
+    for (int m = 0; m < MI; m++)
 #pragma unroll
-      for (int m = 0; m < MI; m++)
+      for (int n = 0; n < NI; n++) acc[m][n] = emm_mfma<T>(fb[0][n], fa[0][m], acc[m][n]);
+    if constexpr (!ANY) emm_wait_stages<P, D - 2>(stages - 2 - t);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();  // stage t + 1 is in LDS, and everyone has read stage t
+    asm volatile("" ::: "memory");
+    emm_traffic<ANY, MI, NI>(a, b, lds + at * STAGE, now, 0, t + 1 < stages, t + (ANY ? 3 : D) < stages, t + 2 < stages, rm, cn, wave, lane, fa[0], fb[0]);
 #pragma unroll
-        for (int n = 0; n < NI; n++) acc[m][n] = emm_mfma<T>(fb[s][n], fa[s][m], acc[m][n]);
-    if constexpr (ANY) {
-      if (t + 1 < stages) {
-        char* then = lds + ((t + 1) & 1) * STAGE;
-        a.put(then, wave, lane);
-        b.put(then + A::BYTES, wave, lane);
-      }
-    }
+    for (int m = 0; m < MI; m++)
+#pragma unroll
+      for (int n = 0; n < NI; n++) acc[m][n] = emm_mfma<T>(fb[1][n], fa[1][m], acc[m][n]);
   }
 }
 
@@ -406,12 +435,12 @@ struct ExpertRowsArgs {
 };
 
 // ACROSS: the weights' rows are the reduction (dX), else they are the output's columns (Y).
-template <typename T, bool ACROSS, bool ANY, int BM, int BN, int WM, int WN>
+template <typename T, bool ACROSS, bool ANY, int BM, int BN, int WM, int WN, int D>
 __global__ __launch_bounds__(64 * WM * WN) void expert_rows_tile_kernel(ExpertRowsArgs p) {
   constexpr int NW = WM * WN, MI = BM / WM / 16, NI = BN / WN / 16;
-  typedef AlongRows<T, BM, NW> OpA;
-  typedef std::conditional_t<ACROSS, AcrossRows<T, BN, NW>, AlongRows<T, BN, NW>> OpB;
-  __shared__ __align__(16) char lds[2 * (OpA::BYTES + OpB::BYTES)];
+  typedef AlongRows<T, BM, NW, true> OpA;
+  typedef std::conditional_t<ACROSS, AcrossRows<T, BN, NW, false>, AlongRows<T, BN, NW, false>> OpB;
+  __shared__ __align__(16) char lds[D * (OpA::BYTES + OpB::BYTES)];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   ExpertTile t;
   if (!expert_tile(p.off, p.E, p.R, BM, p.nt, blockIdx.x, &t)) return;
@@ -422,38 +451,38 @@ __global__ __launch_bounds__(64 * WM * WN) void expert_rows_tile_kernel(ExpertRo
   OpA a;
   OpB b;
   const int64_t ldw = ACROSS ? p.NO : p.Q;
-  const bool owned = e < p.E;
+  const bool owned = e < p.E && p.T > 0;
   if (owned) {
     const int* row = p.row;
     const int last = hi - 1, total = p.T;
     a.begin(static_cast<const T*>(p.A), p.Q, p.Q, wave, lane, [&](int j) -> int64_t {
       const int r = min(m0 + j, last);  // (rows past the expert's: any will do)
-      if (!row) return r;
-      const int s = row[r];
-      return s >= 0 && s < total ? s : -1;
+      return row ? min(max(row[r], 0), total - 1) : r;
     });
     const T* w = static_cast<const T*>(p.W) + (int64_t)e * p.Q * p.NO;
     if constexpr (ACROSS) {
-      b.begin(w, ldw, nullptr, p.Q, p.Q, n0, p.NO, wave, lane);
+      b.template begin<ANY>(w, ldw, nullptr, p.Q, p.Q, n0, p.NO, wave, lane);
     } else {
-      const int cols = p.NO - 1;
-      b.begin(w, ldw, p.Q, wave, lane, [&](int j) -> int64_t { return min(n0 + j, cols); });
+      const int most = p.NO - 1 - n0;
+      b.begin(w + n0 * ldw, ldw, p.Q, wave, lane, [&](int j) -> int64_t { return min(j, most); });
     }
   }
   const int stages = owned ? (p.Q + OpA::BK - 1) / OpA::BK : 0;
-  emm_loop<T, ANY, MI, NI>(a, b, lds, stages, rm, cn, wave, lane, acc);
+  emm_loop<T, ANY, D, MI, NI>(a, b, (lds_char*)lds, stages, rm, cn, wave, lane, acc);
   const int i = lane & 15, q = lane >> 4;
   const bool by4 = (p.NO & 3) == 0;
 #pragma unroll
   for (int m = 0; m < MI; m++) {
     const int r = m0 + rm + 16 * m + i;
     if (r >= hi) continue;
+    const bool nothing = p.row && owned && (p.row[r] < 0 || p.row[r] >= p.T);  // (a row of zeros)
 #pragma unroll
     for (int n = 0; n < NI; n++) {
       const int c = n0 + cn + 16 * n + 4 * q;
       if (c >= p.NO) continue;
       const int64_t o = (int64_t)r * p.NO + c;
       f4 v = acc[m][n];
+      if (nothing) v = f4{0, 0, 0, 0};
       if (p.relu) {
 #pragma unroll
         for (int x = 0; x < 4; x++) v[x] = v[x] > 0.0f ? v[x] : 0.0f;  // (NaN and -0 give +0)
@@ -486,18 +515,17 @@ struct ExpertWeightsArgs {
   int add;
 };
 
-template <typename T, typename TO, bool ANY, int BM, int BN, int WM, int WN>
+template <typename T, typename TO, bool ANY, bool LIST, int BM, int BN, int WM, int WN, int D>
 __global__ __launch_bounds__(64 * WM * WN) void expert_weights_kernel(ExpertWeightsArgs p) {
   constexpr int NW = WM * WN, MI = BM / WM / 16, NI = BN / WN / 16;
-  typedef AcrossRows<T, BM, NW> OpA;
-  typedef AcrossRows<T, BN, NW> OpB;
-  __shared__ __align__(16) char lds[2 * (OpA::BYTES + OpB::BYTES)];
+  typedef AcrossRows<T, BM, NW, false> OpA;
+  typedef AcrossRows<T, BN, NW, LIST> OpB;
+  __shared__ __align__(16) char lds[D * (OpA::BYTES + OpB::BYTES)];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  // every XCD takes a run of tiles of its own
-  const unsigned per = p.mt * p.nt, total = per * p.E, run = (total + 7) / 8;
-  const unsigned at = (blockIdx.x & 7) * run + blockIdx.x / 8;
-  if (blockIdx.x / 8 >= run || at >= total) return;
-  const int e = (int)(at / per), in = (int)(at % per);
+  // every XCD (workgroups equal modulo 8) takes an eighth of each expert's tiles: experts' rows, and with them tiles' times, differ
+  const int per = p.mt * p.nt, share = (per + 7) / 8;
+  const int e = (int)(blockIdx.x / 8) / share, in = (int)(blockIdx.x & 7) * share + (int)(blockIdx.x / 8) % share;
+  if (e >= p.E || in >= per) return;
   const int block = in / (8 * p.nt), rest = in % (8 * p.nt), height = min(8, p.mt - 8 * block);
   const int m0 = (8 * block + rest % height) * BM, n0 = (rest / height) * BN;
   const int lo = min(max(p.off[e], 0), p.R), hi = min(max(p.off[e + 1], 0), p.R), rows = max(hi - lo, 0);
@@ -505,10 +533,10 @@ __global__ __launch_bounds__(64 * WM * WN) void expert_weights_kernel(ExpertWeig
   f4 acc[MI][NI];
   OpA a;
   OpB b;
-  a.begin(static_cast<const T*>(p.dY) + (int64_t)lo * p.N, p.N, nullptr, rows, rows, m0, p.N, wave, lane);
-  if (p.row) b.begin(static_cast<const T*>(p.X), p.K, p.row + lo, rows, p.T, n0, p.K, wave, lane);
-  else b.begin(static_cast<const T*>(p.X) + (int64_t)lo * p.K, p.K, nullptr, rows, rows, n0, p.K, wave, lane);
-  emm_loop<T, ANY, MI, NI>(a, b, lds, (rows + OpA::BK - 1) / OpA::BK, rm, cn, wave, lane, acc);
+  a.template begin<ANY>(static_cast<const T*>(p.dY) + (int64_t)lo * p.N, p.N, nullptr, rows, rows, m0, p.N, wave, lane);
+  if constexpr (LIST) b.template begin<ANY>(static_cast<const T*>(p.X), p.K, p.row + lo, rows, p.T, n0, p.K, wave, lane);
+  else b.template begin<ANY>(static_cast<const T*>(p.X) + (int64_t)lo * p.K, p.K, nullptr, rows, rows, n0, p.K, wave, lane);
+  emm_loop<T, ANY, D, MI, NI>(a, b, (lds_char*)lds, (rows + OpA::BK - 1) / OpA::BK, rm, cn, wave, lane, acc);
   const int i = lane & 15, q = lane >> 4;
   const bool by4 = (p.K & 3) == 0;
   TO* out = static_cast<TO*>(p.dW) + (int64_t)e * p.N * p.K;

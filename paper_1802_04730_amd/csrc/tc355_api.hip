@@ -721,6 +721,7 @@ bool try_gconv_i8_small(const GconvArgs& g, hipStream_t s, tc_status* st) {
 }  // namespace
 
 void tc355::note_path(const char* path) { t_path = path; }
+int tc355::compute_units() { return std::max(1, device_cus()); }
 
 extern "C" {
 

@@ -10,6 +10,8 @@
 
 #include "embed.hpp"
 #include "expert_mm.hpp"
+#include "expert_mm_plan.hpp"
+#include "expert_rows.hpp"
 #include "expert_sum.hpp"
 #include "key_sort.hpp"
 #include "route.hpp"
@@ -20,6 +22,7 @@ using namespace tc355;
 namespace {
 
 constexpr int64_t kMostRows = (int64_t)1 << 30;   // rows, widths: 32-bit indices with room for a tile
+constexpr int64_t kMostWidth = (int64_t)1 << 22;  // of the products: a tile's 256 rows of fp32 within 32-bit offsets
 constexpr int64_t kMostIndex = ((int64_t)1 << 31) - 1;
 
 inline bool misaligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) != 0; }
@@ -153,15 +156,21 @@ int64_t route_ws(int64_t T, int64_t E) {
 
 // ---- products grouped by expert -----------------------------------------------------------------------------------------------
 
-// Row tiles that R rows of E experts can need, whatever their shares, those of no expert among them.
-int64_t most_row_tiles(int64_t R, int64_t E, int64_t bm) { return std::min(R, (R + (E + 1) * (bm - 1)) / bm); }
-
-template <typename T, bool ACROSS, bool ANY, int BM, int BN, int WM, int WN>
+template <typename T, bool ACROSS, bool ANY, int BM, int BN, int WM, int WN, int D>
 tc_status launch_rows_tile(ExpertRowsArgs a, hipStream_t s) {
   a.nt = (int)ceil_div(a.NO, BN);
   const int64_t grid = (most_row_tiles(a.R, a.E, BM) * a.nt + 7) / 8 * 8;
   if (grid > kMostIndex / (64 * WM * WN) * 2) return TC_ERR_UNSUPPORTED;
-  expert_rows_tile_kernel<T, ACROSS, ANY, BM, BN, WM, WN><<<dim3((unsigned)grid), dim3(64 * WM * WN), 0, s>>>(a);
+  expert_rows_tile_kernel<T, ACROSS, ANY, BM, BN, WM, WN, D><<<dim3((unsigned)grid), dim3(64 * WM * WN), 0, s>>>(a);
+  return launched();
+}
+
+template <typename T, int RT, int CT, int WK>
+tc_status launch_few_rows(ExpertRowsArgs a, hipStream_t s) {
+  a.nt = (int)ceil_div(a.NO, 16 * CT);
+  const int64_t grid = (most_row_tiles(a.R, a.E, 16 * RT) * a.nt + 7) / 8 * 8;
+  if (grid > kMostIndex / (64 * WK) * 2) return TC_ERR_UNSUPPORTED;
+  expert_few_rows_kernel<T, RT, CT, WK><<<dim3((unsigned)grid), dim3(64 * WK), 0, s>>>(a);
   return launched();
 }
 
@@ -170,18 +179,39 @@ tc_status run_rows(const ExpertRowsArgs& a, tc_type type, hipStream_t s) {
   return by_type(type, [&](auto t) {
     typedef decltype(t) T;
     const bool whole = (int64_t)a.Q * sizeof(T) % 16 == 0 && (!ACROSS || (int64_t)a.NO * sizeof(T) % 16 == 0);
-    return whole ? launch_rows_tile<T, ACROSS, false, 128, 128, 2, 2>(a, s) : launch_rows_tile<T, ACROSS, true, 128, 128, 2, 2>(a, s);
+    const int most = sizeof(T) == 4 ? 64 : whole && !ACROSS ? 256 : 128;
+    const int side = expert_tile_side(most, compute_units(), [&](int b) { return expected_row_tiles(a.R, a.E, b) * (double)ceil_div(a.NO, b); });
+    if constexpr (sizeof(T) == 2) {
+      if constexpr (!ACROSS)
+        if (side == 256) return launch_rows_tile<T, ACROSS, false, 256, 256, 2, 4, 2>(a, s);
+      if (side == 128) return whole ? launch_rows_tile<T, ACROSS, false, 128, 128, 2, 4, 2>(a, s) : launch_rows_tile<T, ACROSS, true, 128, 128, 2, 4, 2>(a, s);
+    }
+    return whole ? launch_rows_tile<T, ACROSS, false, 64, 64, 2, 2, 3>(a, s) : launch_rows_tile<T, ACROSS, true, 64, 64, 2, 2, 2>(a, s);
   });
 }
 
-template <typename T, typename TO, bool ANY, int BM, int BN, int WM, int WN>
-tc_status launch_weights(ExpertWeightsArgs a, hipStream_t s) {
+template <typename T, typename TO, bool ANY, bool LIST, int BM, int BN, int WM, int WN, int D>
+tc_status launch_weights_list(ExpertWeightsArgs a, hipStream_t s) {
   a.mt = (int)ceil_div(a.N, BM);
   a.nt = (int)ceil_div(a.K, BN);
-  if (prod_reaches({a.mt, a.nt, a.E}, kMostIndex / (64 * WM * WN) * 2)) return TC_ERR_UNSUPPORTED;
-  const int64_t grid = ((int64_t)a.mt * a.nt * a.E + 7) / 8 * 8;
-  expert_weights_kernel<T, TO, ANY, BM, BN, WM, WN><<<dim3((unsigned)grid), dim3(64 * WM * WN), 0, s>>>(a);
+  const int64_t share = ceil_div((int64_t)a.mt * a.nt, 8);
+  if (prod_reaches({share, 8, a.E}, kMostIndex / (64 * WM * WN) * 2)) return TC_ERR_UNSUPPORTED;
+  const int64_t grid = 8 * share * a.E;
+  expert_weights_kernel<T, TO, ANY, LIST, BM, BN, WM, WN, D><<<dim3((unsigned)grid), dim3(64 * WM * WN), 0, s>>>(a);
   return launched();
+}
+template <typename T, typename TO, bool ANY, int B, int WM, int WN, int D>
+tc_status launch_weights(const ExpertWeightsArgs& a, hipStream_t s) {
+  return a.row ? launch_weights_list<T, TO, ANY, true, B, B, WM, WN, D>(a, s) : launch_weights_list<T, TO, ANY, false, B, B, WM, WN, D>(a, s);
+}
+template <typename T, typename TO>
+tc_status run_weights(const ExpertWeightsArgs& a, hipStream_t s) {
+  const bool whole = (int64_t)a.N * sizeof(T) % 16 == 0 && (int64_t)a.K * sizeof(T) % 16 == 0;
+  const int side = expert_tile_side(sizeof(T) == 4 ? 64 : 128, compute_units(),
+                                    [&](int b) { return (double)a.E * (double)ceil_div(a.N, b) * (double)ceil_div(a.K, b); });
+  if constexpr (sizeof(T) == 2)
+    if (side == 128) return whole ? launch_weights<T, TO, false, 128, 2, 4, 2>(a, s) : launch_weights<T, TO, true, 128, 2, 4, 2>(a, s);
+  return whole ? launch_weights<T, TO, false, 64, 2, 2, 3>(a, s) : launch_weights<T, TO, true, 64, 2, 2, 2>(a, s);
 }
 
 }  // namespace
@@ -319,10 +349,17 @@ tc_status tc_expert_mm(const void* X, const void* W, const int32_t* Off, const i
   if (!W || !Off || (R && (!Y || (T && !X)))) return TC_ERR_NULL;
   if (R && (Y == X || Y == W || Y == static_cast<const void*>(Off) || Y == static_cast<const void*>(Row))) return TC_ERR_ALIAS;
   if (misaligned(X) || misaligned(W) || misaligned(Off) || misaligned(Row) || misaligned(Y)) return TC_ERR_ALIGN;
-  if (T >= kMostRows || R >= kMostRows || E >= kMostRows || N >= kMostRows || K >= kMostRows) return TC_ERR_UNSUPPORTED;
+  if (T >= kMostRows || R >= kMostRows || E >= kMostRows || N >= kMostWidth || K >= kMostWidth) return TC_ERR_UNSUPPORTED;
   if (R == 0) return TC_OK;
   const ExpertRowsArgs a{X, W, Y, nullptr, Off, Row, (int)R, (int)T, (int)E, (int)K, (int)N, 0, relu != 0};
-  return took("expert_mm:tile", run_rows<false>(a, type, static_cast<hipStream_t>(hip_stream)));
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  const int64_t share = R / E;
+  if (share < 64)
+    return took("expert_mm:rows", by_type(type, [&](auto t) {
+                  typedef decltype(t) T_;
+                  return share < 16 ? launch_few_rows<T_, 1, 2, 4>(a, s) : launch_few_rows<T_, 4, 2, 4>(a, s);
+                }));
+  return took("expert_mm:tile", run_rows<false>(a, type, s));
 }
 
 tc_status tc_expert_mm_grad_x(const void* dY, const void* W, const int32_t* Off, const void* gate, void* dX, int64_t R, int64_t E, int64_t N, int64_t K,
@@ -331,7 +368,7 @@ tc_status tc_expert_mm_grad_x(const void* dY, const void* W, const int32_t* Off,
   if (!W || !Off || (R && (!dY || !dX))) return TC_ERR_NULL;
   if (R && (dX == dY || dX == W || dX == static_cast<const void*>(Off) || dX == gate)) return TC_ERR_ALIAS;
   if (misaligned(dY) || misaligned(W) || misaligned(Off) || misaligned(gate) || misaligned(dX)) return TC_ERR_ALIGN;
-  if (R >= kMostRows || E >= kMostRows || N >= kMostRows || K >= kMostRows) return TC_ERR_UNSUPPORTED;
+  if (R >= kMostRows || E >= kMostRows || N >= kMostWidth || K >= kMostWidth) return TC_ERR_UNSUPPORTED;
   if (R == 0) return TC_OK;
   const ExpertRowsArgs a{dY, W, dX, gate, Off, nullptr, (int)R, (int)R, (int)E, (int)N, (int)K, 0, 0};
   return took("expert_mm_grad_x:tile", run_rows<true>(a, type, static_cast<hipStream_t>(hip_stream)));
@@ -351,16 +388,13 @@ tc_status tc_expert_mm_grad_w(const void* dY, const void* X, const int32_t* Off,
   if (workspace && (workspace == dY || workspace == X || workspace == dW || workspace == static_cast<const void*>(Off) || workspace == static_cast<const void*>(Row)))
     return TC_ERR_ALIAS;
   if (misaligned(dY) || misaligned(X) || misaligned(Off) || misaligned(Row) || misaligned(dW) || misaligned(workspace)) return TC_ERR_ALIGN;
-  if (T >= kMostRows || R >= kMostRows || E >= kMostRows || N >= kMostRows || K >= kMostRows) return TC_ERR_UNSUPPORTED;
+  if (T >= kMostRows || R >= kMostRows || E >= kMostRows || N >= kMostWidth || K >= kMostWidth) return TC_ERR_UNSUPPORTED;
   if (R == 0 && add) return TC_OK;
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   ExpertWeightsArgs a{dY, X, dW, Off, Row, (int)R, (int)T, (int)E, (int)N, (int)K, 0, 0, add != 0};
   return took("expert_mm_grad_w:tile", by_type(type, [&](auto t) {
                 typedef decltype(t) T_;
-                const bool whole = N * (int64_t)sizeof(T_) % 16 == 0 && K * (int64_t)sizeof(T_) % 16 == 0;
-                if (grad_type == TC_F32)
-                  return whole ? launch_weights<T_, float, false, 128, 128, 2, 2>(a, s) : launch_weights<T_, float, true, 128, 128, 2, 2>(a, s);
-                return whole ? launch_weights<T_, T_, false, 128, 128, 2, 2>(a, s) : launch_weights<T_, T_, true, 128, 128, 2, 2>(a, s);
+                return grad_type == TC_F32 ? run_weights<T_, float>(a, s) : run_weights<T_, T_>(a, s);
               }));
 }
 

@@ -7,6 +7,8 @@ namespace tc355 {
 
 // Sets what tc355_last_path returns on this thread (a string that lives on); in tc355_api.hip.
 void note_path(const char* path);
+// Compute units of the current device; in tc355_api.hip.
+int compute_units();
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
