@@ -103,9 +103,9 @@ __device__ __forceinline__ bool expert_tile(const int* off, int E, int R, int bm
 template <typename T>
 __device__ __forceinline__ u4 emm_load_any(const T* p, int left) {
   constexpr int PER = Elem<T>::PER16;
-  Any16<T> v;
+  Pack<T, PER> v;
   if (left >= PER) {
-    v = load16(p);
+    v = load_pack<T, PER>(p);
   } else {
 #pragma unroll
     for (int i = 0; i < PER; i++) v.e[i] = i < left ? p[i] : static_cast<T>(0.0f);

@@ -41,13 +41,13 @@ __global__ __launch_bounds__(64 * WK) void expert_few_rows_kernel(ExpertRowsArgs
     int s = first;
     const int end = min(last, whole);
     for (; s + U <= end; s += U) {
-      Any16<T> fb[U][CT], fa[U][RT];
+      Pack<T, PER> fb[U][CT], fa[U][RT];
 #pragma unroll
       for (int u = 0; u < U; u++) {
 #pragma unroll
-        for (int n = 0; n < CT; n++) fb[u][n] = load16(b[n] + u * STEP);
+        for (int n = 0; n < CT; n++) fb[u][n] = load_pack<T, PER>(b[n] + u * STEP);
 #pragma unroll
-        for (int m = 0; m < RT; m++) fa[u][m] = load16(a[m] + u * STEP);
+        for (int m = 0; m < RT; m++) fa[u][m] = load_pack<T, PER>(a[m] + u * STEP);
       }
 #pragma unroll
       for (int u = 0; u < U; u++)

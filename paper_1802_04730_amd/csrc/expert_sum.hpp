@@ -6,6 +6,8 @@
 // no part.  The gradient gives a token to one wavefront, which reads its row of dO once for all slots (for 8 of them at
 // a time) and sums dw over its lanes in a fixed order.
 #pragma once
+#include <type_traits>
+
 #include "expert_types.hpp"
 
 namespace tc355 {
@@ -19,53 +21,39 @@ struct ExpertSumArgs {
   int N, k, lpr, cols;
 };
 
-constexpr int ESUM_SLOTS = 8;
-
-template <typename T>
+template <typename T, int V, int SLOTS>
 __global__ __launch_bounds__(WG_THREADS) void expert_sum_kernel(ExpertSumArgs p) {
-  constexpr int V = Elem<T>::PER16;
   typedef typename Wide<T>::type S;
   const int64_t g = ((int64_t)blockIdx.x * WG_THREADS + threadIdx.x) / p.lpr;
   const int64_t t = g / p.cols;
-  if (t >= p.T) return;
-  const int c = ((int)(g % p.cols) * p.lpr + (threadIdx.x & (p.lpr - 1))) * V;
-  if (c >= p.N) return;
-  const bool whole = c + V <= p.N;
-  const T* Y = static_cast<const T*>(p.Y) + c;
+  const RowUnit<V> u((g % p.cols) * p.lpr + (threadIdx.x & (p.lpr - 1)), p.N);
+  if (t >= p.T || !u.on) return;
   S acc[V];
 #pragma unroll
   for (int i = 0; i < V; i++) acc[i] = 0;
-  for (int i0 = 0; i0 < p.k; i0 += ESUM_SLOTS) {
-    long long at[ESUM_SLOTS];
-    float w[ESUM_SLOTS];
+  for (int i0 = 0; i0 < p.k && p.R; i0 += SLOTS) {
+    int64_t at[SLOTS];
+    float w[SLOTS];
+    bool on[SLOTS];
 #pragma unroll
-    for (int j = 0; j < ESUM_SLOTS; j++) {
-      at[j] = i0 + j < p.k ? p.Place[t * p.k + i0 + j] : -1;
-      w[j] = i0 + j < p.k && p.Wt ? p.Wt[t * p.k + i0 + j] : 1.0f;
+    for (int j = 0; j < SLOTS; j++) {
+      const int i = min(i0 + j, p.k - 1), r = p.Place[t * p.k + i];
+      w[j] = p.Wt ? p.Wt[t * p.k + i] : 1.0f;
+      on[j] = i0 + j < p.k && r >= 0 && r < p.R;
+      at[j] = on[j] ? (int64_t)r * p.N : 0;
     }
-    Any16<T> v[ESUM_SLOTS];
-    if (whole) {
+    Pack<T, V> v[SLOTS];  // (a slot that takes no part reads the first row: branches would make each load wait for the one before)
 #pragma unroll
-      for (int j = 0; j < ESUM_SLOTS; j++)
-        if (at[j] >= 0 && at[j] < p.R) v[j] = load16(Y + at[j] * p.N);
-    }
+    for (int j = 0; j < SLOTS; j++) v[j] = load_unit<T, V>(static_cast<const T*>(p.Y) + at[j], u);
 #pragma unroll
-    for (int j = 0; j < ESUM_SLOTS; j++)
-      if (at[j] >= 0 && at[j] < p.R) {
+    for (int j = 0; j < SLOTS; j++)
 #pragma unroll
-        for (int i = 0; i < V; i++)
-          if (whole || c + i < p.N) acc[i] += (S)w[j] * (S)(whole ? v[j].e[i] : Y[at[j] * p.N + i]);
-      }
+      for (int i = 0; i < V; i++) acc[i] = on[j] ? acc[i] + (S)w[j] * (S)v[j].e[i] : acc[i];
   }
-  T* out = static_cast<T*>(p.O) + t * p.N + c;
-  if (whole) {
-    Any16<T> o;
+  Pack<T, V> o;
 #pragma unroll
-    for (int i = 0; i < V; i++) o.e[i] = narrow<T>(acc[i]);
-    store16(out, o);
-  } else {
-    for (int i = 0; c + i < p.N; i++) out[i] = narrow<T>(acc[i]);
-  }
+  for (int i = 0; i < V; i++) o.e[i] = narrow<T>(acc[i]);
+  store_unit<T, V>(static_cast<T*>(p.O) + t * p.N, u, o);
 }
 
 struct ExpertSumGradArgs {
@@ -79,14 +67,17 @@ struct ExpertSumGradArgs {
   int N, k;
 };
 
-template <typename T, int SLOTS>
+template <typename T, int V, int SLOTS>
 __global__ __launch_bounds__(WG_THREADS) void expert_sum_grad_kernel(ExpertSumGradArgs p) {
-  constexpr int V = Elem<T>::PER16;
   typedef typename Wide<T>::type S;
   const int lane = threadIdx.x & 63;
   const int64_t t = (int64_t)blockIdx.x * WAVES_PER_WG + (threadIdx.x >> 6);
   if (t >= p.T) return;
   const T* dO = static_cast<const T*>(p.dO) + t * p.N;
+  if (p.R == 0) {
+    for (int i = lane; i < p.k; i += 64) p.dWt[t * p.k + i] = 0.0f;
+    return;
+  }
   for (int i0 = 0; i0 < p.k; i0 += SLOTS) {
     long long at[SLOTS];
     float w[SLOTS];
@@ -98,35 +89,30 @@ __global__ __launch_bounds__(WG_THREADS) void expert_sum_grad_kernel(ExpertSumGr
       w[j] = i0 + j < p.k ? p.Wt[t * p.k + i0 + j] : 0.0f;
       dw[j] = 0;
     }
-    for (int c = lane * V; c < p.N; c += 64 * V) {
-      if (c + V <= p.N) {
-        const Any16<T> d = load16(dO + c);
-        Any16<T> y[SLOTS];
+    const auto columns = [&](const RowUnit<V>& u, auto whole) {
+      const Pack<T, V> d = load_unit<T, V>(dO, u);
+      Pack<T, V> y[SLOTS];
 #pragma unroll
-        for (int j = 0; j < SLOTS; j++)
-          if (at[j] >= 0) y[j] = load16(static_cast<const T*>(p.Y) + at[j] * p.N + c);
+      for (int j = 0; j < SLOTS; j++)
+        if (at[j] >= 0) y[j] = load_unit<T, V>(static_cast<const T*>(p.Y) + at[j] * p.N, u);
 #pragma unroll
-        for (int j = 0; j < SLOTS; j++)
-          if (at[j] >= 0) {
-            Any16<T> o;
+      for (int j = 0; j < SLOTS; j++)
+        if (at[j] >= 0) {
+          Pack<T, V> o;
 #pragma unroll
-            for (int i = 0; i < V; i++) {
-              dw[j] += (S)d.e[i] * (S)y[j].e[i];
-              o.e[i] = narrow<T>((S)w[j] * (S)d.e[i]);
-            }
-            store16(static_cast<T*>(p.dY) + at[j] * p.N + c, o);
+          for (int i = 0; i < V; i++) {
+            if (whole.value || i >= u.skip) dw[j] += (S)d.e[i] * (S)y[j].e[i];
+            o.e[i] = narrow<T>((S)w[j] * (S)d.e[i]);
           }
-      } else {
-        for (int i = 0; c + i < p.N; i++) {
-          const S d = (S)dO[c + i];
-#pragma unroll
-          for (int j = 0; j < SLOTS; j++)
-            if (at[j] >= 0) {
-              dw[j] += d * (S)static_cast<const T*>(p.Y)[at[j] * p.N + c + i];
-              static_cast<T*>(p.dY)[at[j] * p.N + c + i] = narrow<T>((S)w[j] * d);
-            }
+          T* out = static_cast<T*>(p.dY) + at[j] * p.N;
+          if constexpr (whole.value) store_pack<T, V>(out + u.c, o);
+          else store_unit<T, V>(out, u, o);
         }
-      }
+    };
+    for (int64_t x = lane; x * V < p.N; x += 64) {
+      const RowUnit<V> u(x, p.N);
+      if (u.skip == 0) columns(u, std::true_type{});
+      else columns(u, std::false_type{});
     }
 #pragma unroll
     for (int j = 0; j < SLOTS; j++)

@@ -28,19 +28,48 @@ template <> struct Elem<f16> {
   static constexpr int PER16 = 8;
 };
 
-// 16 bytes whose elements alone are aligned: one load or store all the same (global memory).
-template <typename T>
-struct __attribute__((packed, aligned(sizeof(T)))) Any16 {
-  T e[16 / sizeof(T)];
+// V neighbours whose elements alone are aligned: one load or store of up to 16 bytes all the same (global memory).
+template <typename T, int V>
+struct __attribute__((packed, aligned(sizeof(T)))) Pack {
+  T e[V];
 };
-
-template <typename T>
-__device__ __forceinline__ Any16<T> load16(const T* p) {
-  return *reinterpret_cast<const Any16<T>*>(p);
+template <typename T, int V>
+__device__ __forceinline__ Pack<T, V> load_pack(const T* p) {
+  return *reinterpret_cast<const Pack<T, V>*>(p);
 }
-template <typename T>
-__device__ __forceinline__ void store16(T* p, const Any16<T>& v) {
-  *reinterpret_cast<Any16<T>*>(p) = v;
+template <typename T, int V>
+__device__ __forceinline__ void store_pack(T* p, const Pack<T, V>& v) {
+  *reinterpret_cast<Pack<T, V>*>(p) = v;
+}
+
+// The columns of a row of `width` (at least V) that unit `u` of V handles.  The last unit of a width that is no multiple of V begins V
+// before the end: what it loads is whole, without a branch -- which would make each load wait for the one before --, and it owns the
+// elements from `skip` on.  (Rows narrower than 16 bytes go by units of one element.)
+template <int V>
+struct RowUnit {
+  int c, skip;
+  bool on;
+  __device__ __forceinline__ RowUnit(int64_t u, int width) {
+    const int64_t at = u * V;
+    on = at < width;
+    c = (int)(on ? at : 0);
+    skip = max(0, c + V - width);
+    c -= skip;
+  }
+};
+template <typename T, int V>
+__device__ __forceinline__ Pack<T, V> load_unit(const T* row, const RowUnit<V>& u) {
+  return load_pack<T, V>(row + u.c);
+}
+template <typename T, int V>
+__device__ __forceinline__ void store_unit(T* row, const RowUnit<V>& u, const Pack<T, V>& v) {
+  if (u.skip == 0) {
+    store_pack<T, V>(row + u.c, v);
+  } else {
+#pragma unroll
+    for (int i = 1; i < V; i++)
+      if (i >= u.skip) row[u.c + i] = v.e[i];
+  }
 }
 
 // What a kernel that only streams sums in: float storage in 64 bits, as everywhere in the library; 16-bit storage in 32.

@@ -4,8 +4,9 @@
 // anywhere, of the same digit in earlier workgroups, in earlier wavefronts of its own, in earlier lanes -- and writes them there.
 // No atomics on memory: the order, and with it every sum taken along it, is the same each time.
 //
-// Lanes of one digit find each other by a ballot per bit of the digit.  One digit costs a launch or two and is bounded by their
-// latency at the sizes of a training step (32768 keys: 4 launches); up to SORT_SMALL keys everything stays in one workgroup's LDS, in one launch.
+// Lanes of one digit find each other by a ballot per bit of the digit.  Bounded by the latency of a pass's launches at the sizes of a
+// training step (32768 keys of 18 bits: two passes of two launches, SORT_TIME_LARGE); up to SORT_SMALL keys everything stays in one workgroup's LDS, in
+// one launch (1500 keys of 14 bits: SORT_TIME_SMALL).
 #pragma once
 #include "tc355_device.hpp"
 
@@ -13,10 +14,12 @@ namespace tc355 {
 
 constexpr int SORT_MOST_BITS = 10;          // of a digit
 constexpr int SORT_MOST_BINS = 1 << SORT_MOST_BITS;
-constexpr int SORT_THREADS = 256;
+constexpr int SORT_THREADS = 512;
 constexpr int SORT_TILE = 2048;             // keys of a workgroup
+constexpr int SORT_ROUNDS = 4;              // keys of a thread
 constexpr int SORT_SMALL = 4096;            // keys that one workgroup sorts by itself
-constexpr int SORT_DIRECT_TILES = 64;       // up to so many workgroups add the earlier ones' counts up themselves
+constexpr int SORT_DIRECT_TILES = 32;       // up to so many workgroups add the earlier ones' counts up themselves
+static_assert(SORT_TILE == SORT_ROUNDS * SORT_THREADS && SORT_SMALL == SORT_ROUNDS * 1024, "keys of a workgroup");
 
 // Lanes of the wavefront that have the same digit (of `bits` bits) as this one, among `on`.
 __device__ __forceinline__ unsigned long long same_digit(int d, int bits, bool on) {
@@ -72,10 +75,10 @@ struct SortPass {
   const int* order; // [n]; nullptr in the first pass: 0 .. n-1
   int* key_out;     // [n]
   int* order_out;   // [n]
-  int* count;       // [tiles][bins]
+  int* count;       // [bins][tiles + 1]
   int n, E, shift, bits, tiles;
   long long pad;
-  int summed;       // count holds sums over the earlier tiles; the row behind the last one, all tiles' sums
+  int summed;       // count holds sums over the earlier tiles; behind the last one, all tiles' sum
 };
 
 __device__ __forceinline__ int sort_key(const SortPass& p, int i) {
@@ -93,31 +96,31 @@ static __global__ __launch_bounds__(SORT_THREADS) void sort_count_kernel(SortPas
   for (int j = threadIdx.x; j < SORT_TILE; j += SORT_THREADS)
     if (first + j < p.n) atomicAdd(&count[(sort_key(p, (int)(first + j)) >> p.shift) & (bins - 1)], 1);
   __syncthreads();
-  for (int b = threadIdx.x; b < bins; b += SORT_THREADS) p.count[(int64_t)blockIdx.x * bins + b] = count[b];
+  for (int b = threadIdx.x; b < bins; b += SORT_THREADS) p.count[(int64_t)b * (p.tiles + 1) + blockIdx.x] = count[b];
 }
 
-// count[t][b] of tile t becomes the sum over the tiles before it; count[tiles][b] the sum of all.
-static __global__ __launch_bounds__(64) void sort_sum_kernel(int* count, int tiles, int bins) {
-  const int b = blockIdx.x * 64 + threadIdx.x;
-  if (b >= bins) return;
-  int sum = 0;
-  int t = 0;
-  for (; t + 8 <= tiles; t += 8) {
-    int c[8];
+// count[b][t] of tile t becomes the sum over the tiles before it; count[b][tiles] the sum of all.  A workgroup per bin.
+static __global__ __launch_bounds__(WG_THREADS) void sort_sum_kernel(int* count, int tiles) {
+  __shared__ int part[WAVES_PER_WG];
+  int* c = count + (int64_t)blockIdx.x * (tiles + 1);
+  int run = 0;
+  for (int t0 = 0; t0 < tiles; t0 += 4 * WG_THREADS) {
+    const int t = t0 + 4 * (int)threadIdx.x;
+    int v[4], all = 0, sum;
 #pragma unroll
-    for (int j = 0; j < 8; j++) c[j] = count[(int64_t)(t + j) * bins + b];
-#pragma unroll
-    for (int j = 0; j < 8; j++) {
-      count[(int64_t)(t + j) * bins + b] = sum;
-      sum += c[j];
+    for (int j = 0; j < 4; j++) {
+      v[j] = t + j < tiles ? c[t + j] : 0;
+      all += v[j];
     }
+    int before = run + block_prefix<WAVES_PER_WG>(all, part, &sum);
+#pragma unroll
+    for (int j = 0; j < 4; j++) {
+      if (t + j < tiles) c[t + j] = before;
+      before += v[j];
+    }
+    run += sum;
   }
-  for (; t < tiles; t++) {
-    const int c = count[(int64_t)t * bins + b];
-    count[(int64_t)t * bins + b] = sum;
-    sum += c;
-  }
-  count[(int64_t)tiles * bins + b] = sum;
+  if (threadIdx.x == 0) c[tiles] = run;
 }
 
 // start[b], b < bins: where the first key of tile `tile` with digit b goes.
@@ -128,14 +131,20 @@ __device__ __forceinline__ void tile_starts(const int* count, int tiles, int bin
     const int b = b0 + threadIdx.x;
     int all = 0, before = 0;
     if (b < bins) {
+      const int* c = count + (int64_t)b * (tiles + 1);
       if (summed) {
-        before = count[(int64_t)tile * bins + b];
-        all = count[(int64_t)tiles * bins + b];
+        before = c[tile];
+        all = c[tiles];
       } else {
-        for (int t = 0; t < tiles; t++) {
-          const int c = count[(int64_t)t * bins + b];
-          all += c;
-          before += t < tile ? c : 0;
+        for (int t0 = 0; t0 < tiles; t0 += 8) {
+          int v[8];
+#pragma unroll
+          for (int j = 0; j < 8; j++) v[j] = t0 + j < tiles ? c[t0 + j] : 0;
+#pragma unroll
+          for (int j = 0; j < 8; j++) {
+            all += v[j];
+            before += t0 + j < tile ? v[j] : 0;
+          }
         }
       }
     }
@@ -148,7 +157,7 @@ __device__ __forceinline__ void tile_starts(const int* count, int tiles, int bin
 }
 
 static __global__ __launch_bounds__(SORT_THREADS) void sort_scatter_kernel(SortPass p) {
-  constexpr int WAVES = SORT_THREADS / 64, ROUNDS = SORT_TILE / SORT_THREADS;
+  constexpr int WAVES = SORT_THREADS / 64, ROUNDS = SORT_ROUNDS;
   __shared__ int start[SORT_MOST_BINS], count[WAVES][SORT_MOST_BINS], part[WAVES];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, bins = 1 << p.bits;
   for (int b = lane; b < bins; b += 64) count[wave][b] = 0;
@@ -171,14 +180,15 @@ static __global__ __launch_bounds__(SORT_THREADS) void sort_scatter_kernel(SortP
   }
 }
 
-// All digits in one workgroup, n <= SORT_SMALL.
-static __global__ __launch_bounds__(1024) void sort_small_kernel(SortPass p, int key_bits) {
-  constexpr int WAVES = 16, ROUNDS = SORT_SMALL / 1024;
-  extern __shared__ int mem[];  // keys, indices: SORT_SMALL each; counters: WAVES * bins; starts: bins
+// All digits in one workgroup, n <= SORT_ROUNDS * THREADS.
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void sort_small_kernel(SortPass p, int key_bits) {
+  constexpr int WAVES = THREADS / 64, ROUNDS = SORT_ROUNDS, MOST = ROUNDS * THREADS;
+  extern __shared__ int mem[];  // keys, indices: MOST each; counters: WAVES * bins; starts: bins
   __shared__ int part[WAVES];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, bins = 1 << p.bits;
-  int *keys = mem, *idx = mem + SORT_SMALL, *count = mem + 2 * SORT_SMALL, *start = count + WAVES * bins;
-  const int first = wave * (SORT_SMALL / WAVES) + lane;
+  int *keys = mem, *idx = mem + MOST, *count = mem + 2 * MOST, *start = count + WAVES * bins;
+  const int first = wave * (MOST / WAVES) + lane;
   int key[ROUNDS], at[ROUNDS];
 #pragma unroll
   for (int j = 0; j < ROUNDS; j++) {
@@ -186,23 +196,27 @@ static __global__ __launch_bounds__(1024) void sort_small_kernel(SortPass p, int
     key[j] = at[j] < p.n ? sort_key(p, at[j]) : 0;
   }
   for (int shift = 0; shift < key_bits; shift += p.bits) {
-    for (int b = threadIdx.x; b < WAVES * bins; b += 1024) count[b] = 0;
+    for (int b = threadIdx.x; b < WAVES * bins; b += THREADS) count[b] = 0;
     __syncthreads();
     int rank[ROUNDS];
 #pragma unroll
     for (int j = 0; j < ROUNDS; j++) rank[j] = rank_and_count(count + wave * bins, (key[j] >> shift) & (bins - 1), p.bits, first + 64 * j < p.n, lane);
     __syncthreads();
-    int all = 0;  // (bins <= 1024: a thread has one)
-    if ((int)threadIdx.x < bins) {
+    int run = 0;
+    for (int b0 = 0; b0 < bins; b0 += THREADS) {
+      const int b = b0 + (int)threadIdx.x;
+      int c[WAVES], all = 0, sum;
+#pragma unroll
+      for (int w = 0; w < WAVES; w++) c[w] = b < bins ? count[w * bins + b] : 0;
+#pragma unroll
       for (int w = 0; w < WAVES; w++) {
-        const int c = count[w * bins + threadIdx.x];
-        count[w * bins + threadIdx.x] = all;
-        all += c;
+        if (b < bins) count[w * bins + b] = all;
+        all += c[w];
       }
+      const int lower = block_prefix<WAVES>(all, part, &sum);
+      if (b < bins) start[b] = run + lower;
+      run += sum;
     }
-    int sum;
-    const int lower = block_prefix<WAVES>(all, part, &sum);
-    if ((int)threadIdx.x < bins) start[threadIdx.x] = lower;
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < ROUNDS; j++) {

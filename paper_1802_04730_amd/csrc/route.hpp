@@ -9,19 +9,21 @@
 // The selection compares the logits themselves, as integers that order as they do (-0 as +0), so that rounding never decides.
 //
 // A group of 16 lanes (64 for more than 128 experts) takes a token, each lane the logits lane, lane + G, ..: k rounds find the
-// largest of what is left by exchange inside the group.  What bounds it is those rounds' latency, not the logits' bytes.  A workgroup
-// takes ROUTE_TOKENS tokens and counts its slots per expert; a second launch sums the earlier workgroups' counts and places the
-// slots (key_sort.hpp's ranks by ballot).  Up to ROUTE_TOKENS tokens both are one launch.  No atomics on memory; integer ones in LDS.
+// largest of what is left by exchange inside the group (moves between lanes of a row of 16, without LDS).  What bounds it is those
+// rounds' latency, not the logits' bytes.  A workgroup takes ROUTE_TOKENS tokens and counts its slots per expert; the counts are
+// summed over the workgroups, and a last launch places the slots (key_sort.hpp's ranks by ballot).  Up to ROUTE_ALONE tokens
+// all of it is one workgroup's, in one launch.  No atomics on memory; integer ones in LDS.
 #pragma once
 #include "expert_types.hpp"
 #include "key_sort.hpp"
 
 namespace tc355 {
 
-constexpr int ROUTE_TOKENS = 64;      // of a workgroup
+constexpr int ROUTE_TOKENS = 32;      // of a workgroup
+constexpr int ROUTE_ALONE = 64;       // tokens that one workgroup routes by itself
 constexpr int ROUTE_MOST_E = 1023;    // (with the empty slots' bin: 10 bits)
 constexpr int ROUTE_MOST_K = 64;
-constexpr int ROUTE_DIRECT_TILES = 256;
+constexpr int ROUTE_DIRECT_TILES = 16;
 
 struct RouteArgs {
   const void* L;  // [T][E]
@@ -30,8 +32,9 @@ struct RouteArgs {
   int* Off;       // [E+1]
   int* Row;       // [T*k]
   int* Place;     // [T][k]
-  int* count;     // [tiles + 1][bins]; nullptr: one workgroup does it all
+  int* count;     // [bins][tiles + 1]; nullptr: one workgroup does it all
   int T, E, k, norm, bits, tiles, summed;
+  int tokens;     // of a workgroup
 };
 
 __device__ __forceinline__ unsigned route_order(float x) {  // orders as the logits do; 0: -inf
@@ -41,18 +44,32 @@ __device__ __forceinline__ unsigned route_order(float x) {  // orders as the log
   return o - 0x007fffffu;  // (-inf is the lowest: 0x007fffff)
 }
 
-template <int G, typename F>
-__device__ __forceinline__ void group_all(F f) {
-#pragma unroll
-  for (int d = 1; d < G; d *= 2) f(d);
+// f(x, y) over the G lanes of a group, in all of them: y of another lane.  Rows of 16 lanes by moves between lanes, beyond by LDS.
+template <int CTRL, typename X>
+__device__ __forceinline__ X from_lane(X x) {
+  return __builtin_bit_cast(X, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xf, 0xf, true));
 }
+template <int G, typename X, typename F>
+__device__ __forceinline__ X group_all(X x, F f) {
+  x = f(x, from_lane<0xB1>(x));   // lane ^ 1
+  x = f(x, from_lane<0x4E>(x));   // lane ^ 2
+  x = f(x, from_lane<0x141>(x));  // 7 - lane of 8: the other four
+  x = f(x, from_lane<0x140>(x));  // 15 - lane: the other eight
+#pragma unroll
+  for (int d = 16; d < G; d *= 2) x = f(x, __shfl_xor(x, d));
+  return x;
+}
+__device__ __forceinline__ float most_of(float a, float b) { return fmaxf(a, b); }
+__device__ __forceinline__ float sum_of(float a, float b) { return a + b; }
+__device__ __forceinline__ unsigned larger(unsigned a, unsigned b) { return a > b ? a : b; }
+__device__ __forceinline__ int smaller(int a, int b) { return a < b ? a : b; }
 
-// The places of a workgroup's slots: Id of tokens t0 .. t0 + ROUTE_TOKENS, all threads.
+// The places of a workgroup's slots: Id of the tokens of workgroup `tile`, all threads.
 __device__ __forceinline__ void route_place(const RouteArgs& p, int tile, const int* start, int* count) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, bins = 1 << p.bits;
   for (int b = lane; b < bins; b += 64) count[wave * bins + b] = 0;
-  const int64_t first = (int64_t)tile * ROUTE_TOKENS * p.k, all = (int64_t)p.T * p.k;
-  const int64_t last = min(first + (int64_t)ROUTE_TOKENS * p.k, all);
+  const int64_t first = (int64_t)tile * p.tokens * p.k, all = (int64_t)p.T * p.k;
+  const int64_t last = min(first + (int64_t)p.tokens * p.k, all);
   // a quarter of the slots for each wavefront, counted first, then placed
   const int share = ((int)(last - first) + WAVES_PER_WG - 1) / WAVES_PER_WG;
   const int64_t lo = min(first + (int64_t)wave * share, last), hi = min(lo + share, last);
@@ -93,8 +110,8 @@ __global__ __launch_bounds__(WG_THREADS) void route_kernel(RouteArgs p) {
   __syncthreads();
   const int lane = threadIdx.x & (G - 1), group = threadIdx.x / G;
   const T* L = static_cast<const T*>(p.L);
-  for (int r = group; r < ROUTE_TOKENS; r += WG_THREADS / G) {
-    const int64_t t = (int64_t)blockIdx.x * ROUTE_TOKENS + r;
+  for (int r = group; r < p.tokens; r += WG_THREADS / G) {
+    const int64_t t = (int64_t)blockIdx.x * p.tokens + r;
     if (t >= p.T) break;  // (the whole group, and all groups behind it)
     float x[V];
     unsigned key[V];
@@ -106,34 +123,27 @@ __global__ __launch_bounds__(WG_THREADS) void route_kernel(RouteArgs p) {
       key[v] = route_order(x[v]);
       most = fmaxf(most, x[v]);
     }
-    group_all<G>([&](int d) { most = fmaxf(most, __shfl_xor(most, d)); });
+    most = group_all<G>(most, most_of);
     if (most == -__builtin_inff()) most = 0.0f;  // (nothing to choose: every exp is 0, or NaN)
     float sum = 0.0f;
     if (!p.norm) {
 #pragma unroll
       for (int v = 0; v < V; v++) sum += expf(x[v] - most);
-      group_all<G>([&](int d) { sum += __shfl_xor(sum, d); });
+      sum = group_all<G>(sum, sum_of);
     }
     float val = 0.0f;
     int id = -1;
     const int slot_lane = lane;
     for (int i = 0; i < p.k; i++) {
       unsigned best = 0;
+#pragma unroll
+      for (int v = 0; v < V; v++) best = larger(best, key[v]);
+      best = group_all<G>(best, larger);
       int at = 0x7fffffff;
 #pragma unroll
-      for (int v = 0; v < V; v++)
-        if (key[v] > best) {
-          best = key[v];
-          at = v * G + lane;
-        }
-      group_all<G>([&](int d) {
-        const unsigned ob = __shfl_xor(best, d);
-        const int oa = __shfl_xor(at, d);
-        if (ob > best || (ob == best && oa < at)) {
-          best = ob;
-          at = oa;
-        }
-      });
+      for (int v = V - 1; v >= 0; v--)
+        if (key[v] == best) at = v * G + lane;
+      at = group_all<G>(at, smaller);
       float mine = 0.0f;
 #pragma unroll
       for (int v = 0; v < V; v++)
@@ -141,7 +151,7 @@ __global__ __launch_bounds__(WG_THREADS) void route_kernel(RouteArgs p) {
           key[v] = 0;
           mine = x[v];
         }
-      const float chosen = __shfl(mine, best ? at & (G - 1) : 0, G);
+      const float chosen = group_all<G>(mine, [](float a, float b) { return a != 0.0f ? a : b; });  // (the others have 0; so may it)
       const float w = best ? expf(chosen - most) : 0.0f;
       if (p.norm) sum += w;
       if ((i & (G - 1)) == slot_lane) {
@@ -160,7 +170,7 @@ __global__ __launch_bounds__(WG_THREADS) void route_kernel(RouteArgs p) {
   }
   __syncthreads();
   if (p.count) {
-    for (int b = threadIdx.x; b < bins; b += WG_THREADS) p.count[(int64_t)blockIdx.x * bins + b] = mem[b];
+    for (int b = threadIdx.x; b < bins; b += WG_THREADS) p.count[(int64_t)b * (p.tiles + 1) + blockIdx.x] = mem[b];
     return;
   }
   // one workgroup: counts to starts, then the places
@@ -213,7 +223,7 @@ __global__ __launch_bounds__(WG_THREADS) void route_grad_kernel(RouteGradArgs p)
     g[v] = 0.0f;
     chosen[v] = false;
   }
-  group_all<G>([&](int d) { most = fmaxf(most, __shfl_xor(most, d)); });
+  most = group_all<G>(most, most_of);
   if (most == -__builtin_inff()) most = 0.0f;
   for (int i = 0; i < p.k; i++) {
     const int id = p.Id[t * p.k + i];
@@ -232,10 +242,8 @@ __global__ __launch_bounds__(WG_THREADS) void route_grad_kernel(RouteGradArgs p)
     if (!p.norm || chosen[v]) sum += x[v];
     if (chosen[v]) inner += g[v] * x[v];
   }
-  group_all<G>([&](int d) {
-    sum += __shfl_xor(sum, d);
-    inner += __shfl_xor(inner, d);
-  });
+  sum = group_all<G>(sum, sum_of);
+  inner = group_all<G>(inner, sum_of);
   if (sum == 0.0f) sum = 1.0f;  // (a row of nothing, or without slots)
   inner /= sum;
 #pragma unroll

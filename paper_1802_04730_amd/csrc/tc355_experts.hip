@@ -61,8 +61,8 @@ RowLanes row_lanes(int64_t width, int per16) {
 // ---- token tables -----------------------------------------------------------------------------------------------------------
 
 struct EmbedGradPlan {
-  int key_bits, passes, bits;
-  int64_t tiles, stretches;
+  int key_bits, passes, bits, chunk;
+  int64_t tiles, chunks;
   int64_t key_a, order_a, key_b, order_b, count, part, bytes;  // offsets into the workspace
 };
 
@@ -72,7 +72,8 @@ EmbedGradPlan embed_grad_plan(int64_t E, int64_t D, int64_t T) {
   p.passes = (int)ceil_div(p.key_bits, SORT_MOST_BITS);
   p.bits = (int)ceil_div(p.key_bits, p.passes);
   p.tiles = ceil_div(T, SORT_TILE);
-  p.stretches = T / EMBED_RUN;
+  p.chunk = T < 512 * EMBED_CHUNK ? EMBED_SMALL_CHUNK : EMBED_CHUNK;
+  p.chunks = ceil_div(T, p.chunk);
   int64_t at = 0;
   const auto take = [&](int64_t n) {
     const int64_t o = at;
@@ -86,7 +87,7 @@ EmbedGradPlan embed_grad_plan(int64_t E, int64_t D, int64_t T) {
     p.order_b = take(T * 4);
     p.count = take((p.tiles + 1) * ((int64_t)4 << p.bits));
   }
-  p.part = take(p.stretches * D * 8);
+  p.part = take(p.chunks * 2 * D * 8);
   p.bytes = at;
   return p;
 }
@@ -106,8 +107,10 @@ tc_status sort_tokens(const EmbedGradPlan& pl, const int32_t* Idx, int64_t T, in
   if (T <= SORT_SMALL) {
     a.key_out = keys[0];
     a.order_out = orders[0];
-    const size_t lds = (2 * (size_t)SORT_SMALL + 17 * ((size_t)1 << pl.bits)) * 4;
-    sort_small_kernel<<<1, 1024, lds, s>>>(a, pl.key_bits);
+    const auto lds = [&](int threads) { return (2 * (size_t)SORT_ROUNDS * threads + (threads / 64 + 1) * ((size_t)1 << pl.bits)) * 4; };
+    if (T <= SORT_ROUNDS * 256) sort_small_kernel<256><<<1, 256, lds(256), s>>>(a, pl.key_bits);
+    else if (T <= SORT_ROUNDS * 512) sort_small_kernel<512><<<1, 512, lds(512), s>>>(a, pl.key_bits);
+    else sort_small_kernel<1024><<<1, 1024, lds(1024), s>>>(a, pl.key_bits);
     *key = keys[0];
     *order = orders[0];
     return launched();
@@ -120,7 +123,7 @@ tc_status sort_tokens(const EmbedGradPlan& pl, const int32_t* Idx, int64_t T, in
     a.key_out = keys[i & 1];
     a.order_out = orders[i & 1];
     sort_count_kernel<<<tiles, SORT_THREADS, 0, s>>>(a);
-    if (a.summed) sort_sum_kernel<<<(bins + 63) / 64, 64, 0, s>>>(a.count, (int)tiles, (int)bins);
+    if (a.summed) sort_sum_kernel<<<bins, WG_THREADS, 0, s>>>(a.count, (int)tiles);
     sort_scatter_kernel<<<tiles, SORT_THREADS, 0, s>>>(a);
     if (const tc_status st = launched(); st != TC_OK) return st;
     a.key = keys[i & 1];
@@ -151,7 +154,7 @@ tc_status by_lanes(int64_t E, int64_t k, F f) {
 
 int64_t route_ws(int64_t T, int64_t E) {
   const int64_t tiles = ceil_div(T, ROUTE_TOKENS);
-  return tiles <= 1 ? 0 : (tiles + 1) * ((int64_t)4 << bits_of(E));
+  return T <= ROUTE_ALONE ? 0 : (tiles + 1) * ((int64_t)4 << bits_of(E));
 }
 
 // ---- products grouped by expert -----------------------------------------------------------------------------------------------
@@ -228,14 +231,15 @@ tc_status tc_embed(const void* LUT, const int32_t* Idx, void* O, int64_t E, int6
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   return took("embed:rows", by_type(type, [&](auto x) {
                 typedef decltype(x) X;
-                EmbedArgs a{LUT, Idx, O, E, T, (int)D, 0, 0, scale};
-                const RowLanes rl = row_lanes(D, Elem<X>::PER16);
-                a.lpr = rl.lpr;
-                a.cols = rl.cols;
+                constexpr int V = Elem<X>::PER16;
+                const int v = D < V ? 1 : V;
+                const RowLanes rl = row_lanes(D, v);
+                const EmbedArgs a{LUT, Idx, O, E, T, (int)D, rl.lpr, rl.cols, scale};
                 const int64_t all = ceil_div(T * a.cols, WG_THREADS / a.lpr);
                 for (int64_t at = 0; at < all;) {
                   const int64_t n = next_launch(all - at, WG_THREADS);
-                  embed_kernel<X><<<dim3((unsigned)n), dim3(WG_THREADS), 0, s>>>(a, at);
+                  if (v == V) embed_kernel<X, V><<<dim3((unsigned)n), dim3(WG_THREADS), 0, s>>>(a, at);
+                  else embed_kernel<X, 1><<<dim3((unsigned)n), dim3(WG_THREADS), 0, s>>>(a, at);
                   at += n;
                 }
                 return launched();
@@ -260,29 +264,37 @@ tc_status tc_embed_grad(const void* dO, const int32_t* Idx, void* dLUT, int64_t 
   if (T == 0 && add) return TC_OK;
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   char* ws = static_cast<char*>(workspace);
-  return by_type(type, [&](auto x) {
+  const auto run_by = [&](auto x, auto y, auto v) {
     typedef decltype(x) X;
+    typedef decltype(y) Y;
+    constexpr int V = decltype(v)::value;
     EmbedGradArgs a{};
-    const RowLanes rl = row_lanes(D, Elem<X>::PER16);
     a.dO = dO; a.dLUT = dLUT; a.part = T ? ws + pl.part : nullptr;
-    a.T = (int)T; a.E = (int)E; a.D = (int)D; a.lpr = rl.lpr; a.cols = rl.cols; a.scale = scale; a.add = add != 0;
-    const int groups = WG_THREADS / a.lpr;
-    const int64_t stretch_grid = ceil_div(pl.stretches * a.cols, groups);
-    if (stretch_grid > kMostIndex / WG_THREADS * 2) return TC_ERR_UNSUPPORTED;
-    // rows of a workgroup: enough that its bisections are few beside its rows, as long as 2048 workgroups are left
-    int rows = 64;
-    while (rows > 1 && ceil_div(E, rows) < 2048) rows /= 2;
-    a.rows = rows;
+    a.T = (int)T; a.E = (int)E; a.D = (int)D; a.scale = scale; a.add = add != 0; a.chunk = pl.chunk;
+    a.lpr = 1;
+    while (a.lpr < ceil_div(D, V) && a.lpr < WG_THREADS) a.lpr *= 2;
+    a.token_wgs = (unsigned)ceil_div(pl.chunks, WG_THREADS / a.lpr);
+    int64_t rows = EMBED_FILL_ROWS;
+    while (ceil_div(E, rows) > (int64_t)1 << 22) rows *= 2;  // (fewer than 2^32 threads)
+    a.rows = (int)rows;
+    const int64_t grid = a.token_wgs + (add ? 0 : ceil_div(E, rows));
+    if (grid > kMostIndex / WG_THREADS * 2) return TC_ERR_UNSUPPORTED;
     if (T) {
       const tc_status st = sort_tokens(pl, Idx, T, E, pad, ws, &a.key, &a.order, s);
       if (st != TC_OK) return st;
-      if (stretch_grid) embed_stretch_kernel<X><<<dim3((unsigned)stretch_grid), dim3(WG_THREADS), 0, s>>>(a, (int)pl.stretches);
     }
-    const dim3 grid((unsigned)ceil_div(E, rows));
-    if (grad_type == TC_F32) embed_grad_kernel<X, float><<<grid, dim3(WG_THREADS), 0, s>>>(a);
-    else embed_grad_kernel<X, X><<<grid, dim3(WG_THREADS), 0, s>>>(a);
+    embed_grad_kernel<X, Y, V><<<dim3((unsigned)grid), dim3(WG_THREADS), 0, s>>>(a);
+    if (pl.chunks > 1) {
+      const dim3 join((unsigned)ceil_div(pl.chunks, WAVES_PER_WG), (unsigned)std::min<int64_t>(64, ceil_div(ceil_div(D, V), 64)));
+      embed_join_kernel<X, Y, V><<<join, dim3(WG_THREADS), 0, s>>>(a);
+    }
     return took(T <= SORT_SMALL ? "embed_grad:small_sort" : "embed_grad:sort", launched());
-  });
+  };
+  const auto run = [&](auto x, auto y) {
+    constexpr int V = std::min(Elem<decltype(x)>::PER16, Elem<decltype(y)>::PER16);
+    return D < V ? run_by(x, y, std::integral_constant<int, 1>{}) : run_by(x, y, std::integral_constant<int, V>{});
+  };
+  return by_type(type, [&](auto x) { return grad_type == TC_F32 ? run(x, float{}) : run(x, x); });
 }
 
 size_t tc_route_workspace_bytes(int64_t T, int64_t E, int64_t k) {
@@ -307,7 +319,7 @@ tc_status tc_route(const void* L, float* Wt, int32_t* Id, int32_t* Off, int32_t*
   if (need && (!workspace || misaligned(workspace) || workspace_bytes < (size_t)need)) return TC_ERR_WORKSPACE;
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   RouteArgs a{L, Wt, Id, Off, Row, Place, need ? static_cast<int*>(workspace) : nullptr, (int)T, (int)E, (int)k, norm != 0, bits_of(E),
-              (int)std::max<int64_t>(1, ceil_div(T, ROUTE_TOKENS)), 0};
+              need ? (int)ceil_div(T, ROUTE_TOKENS) : 1, 0, need ? ROUTE_TOKENS : ROUTE_ALONE};
   a.summed = a.tiles > ROUTE_DIRECT_TILES;
   const size_t bins = (size_t)4 << a.bits;
   return by_type(type, [&](auto x) {
@@ -315,7 +327,7 @@ tc_status tc_route(const void* L, float* Wt, int32_t* Id, int32_t* Off, int32_t*
       typedef decltype(x) X;
       route_kernel<X, g.value, v.value><<<dim3((unsigned)a.tiles), dim3(WG_THREADS), a.count ? bins : bins * (1 + WAVES_PER_WG), s>>>(a);
       if (!a.count) return took("route:one", launched());
-      if (a.summed) sort_sum_kernel<<<dim3(((1u << a.bits) + 63) / 64), dim3(64), 0, s>>>(a.count, a.tiles, 1 << a.bits);
+      if (a.summed) sort_sum_kernel<<<dim3(1u << a.bits), dim3(WG_THREADS), 0, s>>>(a.count, a.tiles);
       route_place_kernel<<<dim3((unsigned)a.tiles), dim3(WG_THREADS), bins * (1 + WAVES_PER_WG), s>>>(a);
       return took("route:tiles", launched());
     });
@@ -408,13 +420,18 @@ tc_status tc_expert_sum(const void* Y, const float* Wt, const int32_t* Place, vo
   if (T == 0) return TC_OK;
   return took("expert_sum:rows", by_type(type, [&](auto x) {
                 typedef decltype(x) X;
-                ExpertSumArgs a{Y, Wt, Place, O, T, R, (int)N, (int)k, 0, 0};
-                const RowLanes rl = row_lanes(N, Elem<X>::PER16);
-                a.lpr = rl.lpr;
-                a.cols = rl.cols;
+                constexpr int V = Elem<X>::PER16;
+                const RowLanes rl = row_lanes(N, N < V ? 1 : V);
+                const ExpertSumArgs a{Y, Wt, Place, O, T, R, (int)N, (int)k, rl.lpr, rl.cols};
                 const int64_t grid = ceil_div(T * a.cols, WG_THREADS / a.lpr);
                 if (grid > kMostIndex / WG_THREADS * 2) return TC_ERR_UNSUPPORTED;
-                expert_sum_kernel<X><<<dim3((unsigned)grid), dim3(WG_THREADS), 0, static_cast<hipStream_t>(hip_stream)>>>(a);
+                const dim3 g((unsigned)grid), b(WG_THREADS);
+                hipStream_t s = static_cast<hipStream_t>(hip_stream);
+                if (N < V) expert_sum_kernel<X, 1, 4><<<g, b, 0, s>>>(a);
+                else if (k == 1) expert_sum_kernel<X, V, 1><<<g, b, 0, s>>>(a);
+                else if (k == 2) expert_sum_kernel<X, V, 2><<<g, b, 0, s>>>(a);
+                else if (k <= 4) expert_sum_kernel<X, V, 4><<<g, b, 0, s>>>(a);
+                else expert_sum_kernel<X, V, 8><<<g, b, 0, s>>>(a);
                 return launched();
               }));
 }
@@ -439,9 +456,11 @@ tc_status tc_expert_sum_grad(const void* dO, const void* Y, const float* Wt, con
                 if (grid > kMostIndex / WG_THREADS * 2) return TC_ERR_UNSUPPORTED;
                 const dim3 g((unsigned)grid), b(WG_THREADS);
                 hipStream_t s = static_cast<hipStream_t>(hip_stream);
-                if (k <= 2) expert_sum_grad_kernel<X, 2><<<g, b, 0, s>>>(a);
-                else if (k <= 4) expert_sum_grad_kernel<X, 4><<<g, b, 0, s>>>(a);
-                else expert_sum_grad_kernel<X, 8><<<g, b, 0, s>>>(a);
+                constexpr int V = Elem<X>::PER16;
+                if (N < V) expert_sum_grad_kernel<X, 1, 4><<<g, b, 0, s>>>(a);
+                else if (k <= 2) expert_sum_grad_kernel<X, V, 2><<<g, b, 0, s>>>(a);
+                else if (k <= 4) expert_sum_grad_kernel<X, V, 4><<<g, b, 0, s>>>(a);
+                else expert_sum_grad_kernel<X, V, 8><<<g, b, 0, s>>>(a);
                 return launched();
               }));
 }
