@@ -37,9 +37,19 @@ template <typename T, int V>
 __device__ __forceinline__ Pack<T, V> load_pack(const T* p) {
   return *reinterpret_cast<const Pack<T, V>*>(p);
 }
+// Stores pass the caches by: outputs are far larger than those, or read by a later launch (16384 rows of 4096 bfloat16 out of a table: 73 us,
+// so 46; with a launch behind it that reads them back 62 us either way).
 template <typename T, int V>
 __device__ __forceinline__ void store_pack(T* p, const Pack<T, V>& v) {
-  *reinterpret_cast<Pack<T, V>*>(p) = v;
+  constexpr int BYTES = sizeof(T) * V;
+  if constexpr (BYTES == 16 || BYTES == 8) {
+    typedef unsigned words __attribute__((ext_vector_type(BYTES / 4)));
+    typedef unsigned words_any __attribute__((ext_vector_type(BYTES / 4), aligned(sizeof(T))));
+    __builtin_nontemporal_store(static_cast<words_any>(__builtin_bit_cast(words, v)), reinterpret_cast<words_any*>(p));
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; i++) __builtin_nontemporal_store(v.e[i], p + i);
+  }
 }
 
 // The columns of a row of `width` (at least V) that unit `u` of V handles.  The last unit of a width that is no multiple of V begins V
@@ -68,7 +78,7 @@ __device__ __forceinline__ void store_unit(T* row, const RowUnit<V>& u, const Pa
   } else {
 #pragma unroll
     for (int i = 1; i < V; i++)
-      if (i >= u.skip) row[u.c + i] = v.e[i];
+      if (i >= u.skip) __builtin_nontemporal_store(v.e[i], row + u.c + i);
   }
 }
 

@@ -20,6 +20,16 @@ typedef int (*gconv_t)(const float*, const float*, const float*, float*, int64_t
 typedef int (*kron_t)(const float*, const float*, const float*, float*, int64_t, int64_t, int64_t, int64_t, int64_t, void*);
 typedef int (*sconv_t)(const float*, const float*, const float*, float*, int64_t, int64_t, int64_t, int64_t, int64_t, int64_t, int64_t, int64_t, int64_t,
                        void*);
+typedef int (*embed_t)(const void*, const int32_t*, void*, int64_t, int64_t, int64_t, float, int, void*);
+typedef int (*embed_grad_t)(const void*, const int32_t*, void*, int64_t, int64_t, int64_t, float, int64_t, int32_t, int, int, void*, size_t, void*);
+typedef int (*route_t)(const void*, float*, int32_t*, int32_t*, int32_t*, int32_t*, int64_t, int64_t, int64_t, int32_t, int, void*, size_t, void*);
+typedef int (*route_grad_t)(const void*, const int32_t*, const float*, void*, int64_t, int64_t, int64_t, int32_t, int, void*);
+typedef int (*expert_mm_t)(const void*, const void*, const int32_t*, const int32_t*, void*, int64_t, int64_t, int64_t, int64_t, int64_t, int32_t, int, void*);
+typedef int (*expert_mm_grad_x_t)(const void*, const void*, const int32_t*, const void*, void*, int64_t, int64_t, int64_t, int64_t, int, void*);
+typedef int (*expert_mm_grad_w_t)(const void*, const void*, const int32_t*, const int32_t*, void*, int64_t, int64_t, int64_t, int64_t, int64_t, int32_t, int, int,
+                                  void*, size_t, void*);
+typedef int (*expert_sum_t)(const void*, const float*, const int32_t*, void*, int64_t, int64_t, int64_t, int64_t, int, void*);
+typedef int (*expert_sum_grad_t)(const void*, const void*, const float*, const int32_t*, void*, float*, int64_t, int64_t, int64_t, int64_t, int, void*);
 typedef int (*lut_t)(int32_t, const float* const*, const int32_t* const*, float* const*, const int64_t*, const int64_t*, int64_t, int64_t, void*);
 
 constexpr int kMost = 8;  // layers, tables
@@ -242,6 +252,207 @@ PyObject* call_lut(PyObject*, PyObject* const* v, Py_ssize_t n) {
   });
 }
 
+// ---- operators around experts: tensors of one of three storage types (tc_type in include/tc355.h) ----
+
+struct Kind {
+  c10::ScalarType type = c10::kFloat;
+  int code = -1;
+};
+bool kind_of(PyObject* o, Kind* k) {
+  if (!THPVariable_CheckExact(o)) return false;
+  const at::Tensor& t = THPVariable_Unpack(o);
+  if (!t.defined()) return false;
+  k->type = t.scalar_type();
+  k->code = k->type == c10::kFloat ? 0 : k->type == c10::kBFloat16 ? 1 : k->type == c10::kHalf ? 2 : -1;
+  return k->code >= 0;
+}
+bool take(PyObject* o, const Kind& k, int64_t dims, Arg* a) { return take(o, k.type, dims, a); }
+bool take_ints(PyObject* o, int64_t dims, Arg* a) { return take(o, c10::kInt, dims, a); }
+bool take_or_none(PyObject* o, const Kind& k, int64_t dims, Arg* a) { return o == Py_None || take(o, k.type, dims, a); }
+bool take_ints_or_none(PyObject* o, int64_t dims, Arg* a) { return o == Py_None || take(o, c10::kInt, dims, a); }
+bool is(const Arg& a, int64_t rows, int64_t cols) { return a.size[0] == rows && a.size[1] == cols; }
+
+bool number(PyObject* o, float* x) {
+  if (PyFloat_CheckExact(o)) *x = (float)PyFloat_AS_DOUBLE(o);
+  else if (PyLong_CheckExact(o)) *x = (float)PyLong_AsDouble(o);
+  else return false;
+  return !PyErr_Occurred();
+}
+bool whole_number(PyObject* o, int64_t* x) {
+  if (!PyLong_CheckExact(o)) return false;
+  *x = PyLong_AsLongLong(o);
+  return !PyErr_Occurred();
+}
+bool truth(PyObject* o, int32_t* x) {
+  *x = o == Py_True;
+  return o == Py_True || o == Py_False;
+}
+bool workspace_of(PyObject* o, void** p, size_t* n) {
+  Arg a;
+  *p = nullptr;
+  *n = 0;
+  if (o == Py_None) return true;
+  if (!take(o, c10::kByte, 1, &a)) return false;
+  *p = a.data;
+  *n = (size_t)a.size[0];
+  return true;
+}
+inline const int32_t* ints(const Arg& a) { return static_cast<const int32_t*>(a.data); }
+
+// (entry, LUT, Idx, O, scale, stream)
+PyObject* call_embed(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  return guarded([&]() -> int {
+    Kind k;
+    Arg L, I, O;
+    void* s;
+    float scale;
+    if (n != 6 || !kind_of(v[1], &k) || !take(v[1], k, 2, &L) || !take_ints(v[2], 1, &I) || !take(v[3], k, 2, &O) || !number(v[4], &scale) || !stream_of(v[5], &s)) return -1;
+    const int64_t E = L.size[0], D = L.size[1], T = I.size[0];
+    embed_t entry;
+    if (!is(O, T, D) || !entry_of(v[0], &entry)) return -1;
+    return call(entry, (const void*)L.data, ints(I), O.data, E, D, T, scale, k.code, s);
+  });
+}
+
+// (entry, dO, Idx, dLUT, workspace or None, scale, pad, add, stream)
+PyObject* call_embed_grad(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  return guarded([&]() -> int {
+    Kind k, g;
+    Arg d, I, G;
+    void *s, *ws;
+    size_t bytes;
+    float scale;
+    int64_t pad;
+    int32_t add;
+    if (n != 9 || !kind_of(v[1], &k) || !kind_of(v[3], &g) || (g.code != k.code && g.code != 0) || !take(v[1], k, 2, &d) || !take_ints(v[2], 1, &I) ||
+        !take(v[3], g, 2, &G) || !workspace_of(v[4], &ws, &bytes) || !number(v[5], &scale) || !whole_number(v[6], &pad) || !truth(v[7], &add) || !stream_of(v[8], &s))
+      return -1;
+    const int64_t T = d.size[0], D = d.size[1], E = G.size[0];
+    embed_grad_t entry;
+    if (G.size[1] != D || I.size[0] != T || !entry_of(v[0], &entry)) return -1;
+    return call(entry, (const void*)d.data, ints(I), G.data, E, D, T, scale, pad, add, k.code, g.code, ws, bytes, s);
+  });
+}
+
+// (entry, L, Wt, Id, Off, Row, Place, workspace or None, norm, stream)
+PyObject* call_route(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  return guarded([&]() -> int {
+    Kind k;
+    Arg L, W, I, F, R, P;
+    void *s, *ws;
+    size_t bytes;
+    int32_t norm;
+    if (n != 10 || !kind_of(v[1], &k) || !take(v[1], k, 2, &L) || !take(v[2], 2, &W) || !take_ints(v[3], 2, &I) || !take_ints(v[4], 1, &F) || !take_ints(v[5], 1, &R) ||
+        !take_ints(v[6], 2, &P) || !workspace_of(v[7], &ws, &bytes) || !truth(v[8], &norm) || !stream_of(v[9], &s))
+      return -1;
+    const int64_t T = L.size[0], E = L.size[1], top = I.size[1];
+    route_t entry;
+    if (!is(I, T, top) || !is(W, T, top) || !is(P, T, top) || F.size[0] != E + 1 || R.size[0] != T * top || !entry_of(v[0], &entry)) return -1;
+    return call(entry, (const void*)L.data, out(W), (int32_t*)I.data, (int32_t*)F.data, (int32_t*)R.data, (int32_t*)P.data, T, E, top, norm, k.code, ws, bytes, s);
+  });
+}
+
+// (entry, L, Id, dWt, dL, norm, stream)
+PyObject* call_route_grad(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  return guarded([&]() -> int {
+    Kind k;
+    Arg L, I, W, G;
+    void* s;
+    int32_t norm;
+    if (n != 7 || !kind_of(v[1], &k) || !take(v[1], k, 2, &L) || !take_ints(v[2], 2, &I) || !take(v[3], 2, &W) || !take(v[4], k, 2, &G) || !truth(v[5], &norm) ||
+        !stream_of(v[6], &s))
+      return -1;
+    const int64_t T = L.size[0], E = L.size[1], top = I.size[1];
+    route_grad_t entry;
+    if (!is(I, T, top) || !is(W, T, top) || !is(G, T, E) || !entry_of(v[0], &entry)) return -1;
+    return call(entry, (const void*)L.data, ints(I), f(W), G.data, T, E, top, norm, k.code, s);
+  });
+}
+
+// (entry, X, W, Off, Row or None, Y, relu, stream)
+PyObject* call_expert_mm(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  return guarded([&]() -> int {
+    Kind k;
+    Arg X, W, F, Row, Y;
+    void* s;
+    int32_t relu;
+    if (n != 8 || !kind_of(v[1], &k) || !take(v[1], k, 2, &X) || !take(v[2], k, 3, &W) || !take_ints(v[3], 1, &F) || !take_ints_or_none(v[4], 1, &Row) ||
+        !take(v[5], k, 2, &Y) || !truth(v[6], &relu) || !stream_of(v[7], &s))
+      return -1;
+    const int64_t T = X.size[0], K = X.size[1], E = W.size[0], N = W.size[1], R = Y.size[0];
+    expert_mm_t entry;
+    if (W.size[2] != K || F.size[0] != E + 1 || Y.size[1] != N || (Row.size ? Row.size[0] : T) != R || !entry_of(v[0], &entry)) return -1;
+    return call(entry, (const void*)X.data, (const void*)W.data, ints(F), ints(Row), Y.data, T, R, E, N, K, relu, k.code, s);
+  });
+}
+
+// (entry, dY, W, Off, gate or None, dX, stream)
+PyObject* call_expert_mm_grad_x(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  return guarded([&]() -> int {
+    Kind k;
+    Arg d, W, F, g, X;
+    void* s;
+    if (n != 7 || !kind_of(v[1], &k) || !take(v[1], k, 2, &d) || !take(v[2], k, 3, &W) || !take_ints(v[3], 1, &F) || !take_or_none(v[4], k, 2, &g) ||
+        !take(v[5], k, 2, &X) || !stream_of(v[6], &s))
+      return -1;
+    const int64_t R = d.size[0], N = d.size[1], E = W.size[0], K = W.size[2];
+    expert_mm_grad_x_t entry;
+    if (W.size[1] != N || F.size[0] != E + 1 || !is(X, R, K) || (g.size && !is(g, R, K)) || !entry_of(v[0], &entry)) return -1;
+    return call(entry, (const void*)d.data, (const void*)W.data, ints(F), (const void*)g.data, X.data, R, E, N, K, k.code, s);
+  });
+}
+
+// (entry, dY, X, Off, Row or None, dW, workspace or None, add, stream)
+PyObject* call_expert_mm_grad_w(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  return guarded([&]() -> int {
+    Kind k, g;
+    Arg d, X, F, Row, W;
+    void *s, *ws;
+    size_t bytes;
+    int32_t add;
+    if (n != 9 || !kind_of(v[1], &k) || !kind_of(v[5], &g) || (g.code != k.code && g.code != 0) || !take(v[1], k, 2, &d) || !take(v[2], k, 2, &X) ||
+        !take_ints(v[3], 1, &F) || !take_ints_or_none(v[4], 1, &Row) || !take(v[5], g, 3, &W) || !workspace_of(v[6], &ws, &bytes) || !truth(v[7], &add) ||
+        !stream_of(v[8], &s))
+      return -1;
+    const int64_t R = d.size[0], N = d.size[1], T = X.size[0], K = X.size[1], E = W.size[0];
+    expert_mm_grad_w_t entry;
+    if (W.size[1] != N || W.size[2] != K || F.size[0] != E + 1 || (Row.size ? Row.size[0] : T) != R || !entry_of(v[0], &entry)) return -1;
+    return call(entry, (const void*)d.data, (const void*)X.data, ints(F), ints(Row), W.data, T, R, E, N, K, add, k.code, g.code, ws, bytes, s);
+  });
+}
+
+// (entry, Y, Wt or None, Place, O, stream)
+PyObject* call_expert_sum(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  return guarded([&]() -> int {
+    Kind k;
+    Arg Y, W, P, O;
+    void* s;
+    if (n != 6 || !kind_of(v[1], &k) || !take(v[1], k, 2, &Y) || (v[2] != Py_None && !take(v[2], 2, &W)) || !take_ints(v[3], 2, &P) || !take(v[4], k, 2, &O) ||
+        !stream_of(v[5], &s))
+      return -1;
+    const int64_t R = Y.size[0], N = Y.size[1], T = P.size[0], top = P.size[1];
+    expert_sum_t entry;
+    if (!is(O, T, N) || (W.size && !is(W, T, top)) || !entry_of(v[0], &entry)) return -1;
+    return call(entry, (const void*)Y.data, f(W), ints(P), O.data, T, R, top, N, k.code, s);
+  });
+}
+
+// (entry, dO, Y, Wt, Place, dY, dWt, stream)
+PyObject* call_expert_sum_grad(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  return guarded([&]() -> int {
+    Kind k;
+    Arg d, Y, W, P, dY, dW;
+    void* s;
+    if (n != 8 || !kind_of(v[1], &k) || !take(v[1], k, 2, &d) || !take(v[2], k, 2, &Y) || !take(v[3], 2, &W) || !take_ints(v[4], 2, &P) || !take(v[5], k, 2, &dY) ||
+        !take(v[6], 2, &dW) || !stream_of(v[7], &s))
+      return -1;
+    const int64_t R = Y.size[0], N = Y.size[1], T = P.size[0], top = P.size[1];
+    expert_sum_grad_t entry;
+    if (!is(d, T, N) || !is(W, T, top) || !is(dW, T, top) || !is(dY, R, N) || !entry_of(v[0], &entry)) return -1;
+    return call(entry, (const void*)d.data, (const void*)Y.data, f(W), ints(P), dY.data, out(dW), T, R, top, N, k.code, s);
+  });
+}
+
 template <PyObject* (*F)(PyObject*, PyObject* const*, Py_ssize_t)>
 PyMethodDef method(const char* name) {
   return {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(F)), METH_FASTCALL, nullptr};
@@ -249,7 +460,11 @@ PyMethodDef method(const char* name) {
 
 PyMethodDef methods[] = {method<call_tbmm>("tbmm"),   method<call_tbmm_ws>("tbmm_ws"), method<call_mlp>("mlp"),
                          method<call_gconv>("gconv"), method<call_kron>("kron"),       method<call_sconv>("sconv"),
-                         method<call_lut>("lut"),     {nullptr, nullptr, 0, nullptr}};
+                         method<call_lut>("lut"),     method<call_embed>("embed"),     method<call_embed_grad>("embed_grad"),
+                         method<call_route>("route"), method<call_route_grad>("route_grad"), method<call_expert_mm>("expert_mm"),
+                         method<call_expert_mm_grad_x>("expert_mm_grad_x"), method<call_expert_mm_grad_w>("expert_mm_grad_w"),
+                         method<call_expert_sum>("expert_sum"), method<call_expert_sum_grad>("expert_sum_grad"),
+                         {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fast", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

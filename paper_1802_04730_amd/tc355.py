@@ -132,7 +132,8 @@ def _load_fast(L) -> None:
         warnings.warn("the binding's native calls are not available: calls go through ctypes, some microseconds slower (%s)" % e,
                       RuntimeWarning, stacklevel=3)
         return
-    for name in ("tc_tbmm", "tc_tbmm_ws", "tc_mlp_fcrelu", "tc_group_conv", "tc_kron", "tc_sconv2d", "tc_lut"):
+    for name in ("tc_tbmm", "tc_tbmm_ws", "tc_mlp_fcrelu", "tc_group_conv", "tc_kron", "tc_sconv2d", "tc_lut", "tc_embed", "tc_embed_grad", "tc_route",
+                 "tc_route_grad", "tc_expert_mm", "tc_expert_mm_grad_x", "tc_expert_mm_grad_w", "tc_expert_sum", "tc_expert_sum_grad"):
         _AT[name] = ctypes.cast(getattr(L, name), ctypes.c_void_p).value
     _FAST = fast
 
@@ -414,6 +415,10 @@ def _workspace(ws):
 
 def tc_embed(LUT, Idx, O, scale: float = 1.0, stream=None) -> None:
     """O[T,D] = scale * LUT[Idx[T], :] (int32 numbers; one outside [0, E) gives a row of NaN)."""
+    if _FAST is not None:
+        status = _FAST.embed(_AT["tc_embed"], LUT, Idx, O, scale, stream)
+        if status >= 0:
+            return _check(status, "tc_embed")
     l, i, o = _typed(LUT, "LUT", 2), _typed(Idx, "Idx", 1, torch.int32), _typed(O, "O", 2, LUT.dtype)
     (E, D), T = LUT.shape, Idx.shape[0]
     _fit(tuple(O.shape) == (T, D), "tc_embed")
@@ -428,6 +433,10 @@ def tc_embed_grad(dO, Idx, dLUT, workspace, scale: float = 1.0, pad: int = -1, a
     """dLUT[E,D] (+)= scale * the sum of the rows of dO[T,D] whose number Idx[T] is the row's; `pad` and numbers outside [0, E) take no part.
 
     dLUT is of dO's type or float32.  ``workspace``: a uint8 tensor of at least tc_embed_grad_workspace_bytes(E, D, T) bytes."""
+    if _FAST is not None:
+        status = _FAST.embed_grad(_AT["tc_embed_grad"], dO, Idx, dLUT, workspace, scale, pad, add, stream)
+        if status >= 0:
+            return _check(status, "tc_embed_grad")
     d, i, g = _typed(dO, "dO", 2), _typed(Idx, "Idx", 1, torch.int32), _typed(dLUT, "dLUT", 2, None if dLUT.dtype is torch.float32 else dO.dtype)
     (T, D), E = dO.shape, dLUT.shape[0]
     _fit(dLUT.shape[1] == D and Idx.shape[0] == T, "tc_embed_grad")
@@ -443,6 +452,10 @@ def tc_route(L, Wt, Id, Off, Row, Place, workspace=None, norm: bool = False, str
     """Weights Wt[T,k] and numbers Id[T,k] of the k largest of L[T,E], and the slots by expert: Off[E+1], Row[T*k], Place[T,k].
 
     ``workspace``: a uint8 tensor of at least tc_route_workspace_bytes(T, E, k) bytes (None only when that is 0)."""
+    if _FAST is not None:
+        status = _FAST.route(_AT["tc_route"], L, Wt, Id, Off, Row, Place, workspace, norm, stream)
+        if status >= 0:
+            return _check(status, "tc_route")
     i32 = torch.int32
     args = (_typed(L, "L", 2), _typed(Wt, "Wt", 2, torch.float32), _typed(Id, "Id", 2, i32), _typed(Off, "Off", 1, i32), _typed(Row, "Row", 1, i32),
             _typed(Place, "Place", 2, i32))
@@ -454,6 +467,10 @@ def tc_route(L, Wt, Id, Off, Row, Place, workspace=None, norm: bool = False, str
 
 def tc_route_grad(L, Id, dWt, dL, norm: bool = False, stream=None) -> None:
     """dL[T,E]: the gradient of tc_route's weights, from L[T,E], Id[T,k] and dWt[T,k]."""
+    if _FAST is not None:
+        status = _FAST.route_grad(_AT["tc_route_grad"], L, Id, dWt, dL, norm, stream)
+        if status >= 0:
+            return _check(status, "tc_route_grad")
     args = (_typed(L, "L", 2), _typed(Id, "Id", 2, torch.int32), _typed(dWt, "dWt", 2, torch.float32), _typed(dL, "dL", 2, L.dtype))
     (T, E), k = L.shape, Id.shape[1]
     _fit(tuple(Id.shape) == tuple(dWt.shape) == (T, k) and dL.shape == L.shape, "tc_route_grad")
@@ -462,6 +479,10 @@ def tc_route_grad(L, Id, dWt, dL, norm: bool = False, stream=None) -> None:
 
 def tc_expert_mm(X, W, Off, Row, Y, relu: bool = False, stream=None) -> None:
     """Y[R,N]: rows Off[e] .. Off[e+1] are those of X times W[e] ([N,K]), clamped at 0 if relu; row r of X[T,K] is Row[r], or r where Row is None."""
+    if _FAST is not None:
+        status = _FAST.expert_mm(_AT["tc_expert_mm"], X, W, Off, Row, Y, relu, stream)
+        if status >= 0:
+            return _check(status, "tc_expert_mm")
     i32 = torch.int32
     args = (_typed(X, "X", 2), _typed(W, "W", 3, X.dtype), _typed(Off, "Off", 1, i32), None if Row is None else _typed(Row, "Row", 1, i32),
             _typed(Y, "Y", 2, X.dtype))
@@ -472,6 +493,10 @@ def tc_expert_mm(X, W, Off, Row, Y, relu: bool = False, stream=None) -> None:
 
 def tc_expert_mm_grad_x(dY, W, Off, gate, dX, stream=None) -> None:
     """dX[R,K]: the rows of each expert of dY[R,N] times W[e] ([N,K]); 0 where gate[R,K] (or None) is not above 0."""
+    if _FAST is not None:
+        status = _FAST.expert_mm_grad_x(_AT["tc_expert_mm_grad_x"], dY, W, Off, gate, dX, stream)
+        if status >= 0:
+            return _check(status, "tc_expert_mm_grad_x")
     args = (_typed(dY, "dY", 2), _typed(W, "W", 3, dY.dtype), _typed(Off, "Off", 1, torch.int32), None if gate is None else _typed(gate, "gate", 2, dY.dtype),
             _typed(dX, "dX", 2, dY.dtype))
     (R, N), (E, N2, K) = dY.shape, W.shape
@@ -488,6 +513,10 @@ def tc_expert_mm_grad_w(dY, X, Off, Row, dW, workspace=None, add: bool = False, 
 
     dW is of dY's type or float32.  ``workspace``: as tc_tbmm_ws; less than tc_expert_mm_grad_w_workspace_bytes(R, E, N, K) bytes
     only cost time."""
+    if _FAST is not None:
+        status = _FAST.expert_mm_grad_w(_AT["tc_expert_mm_grad_w"], dY, X, Off, Row, dW, workspace, add, stream)
+        if status >= 0:
+            return _check(status, "tc_expert_mm_grad_w")
     i32 = torch.int32
     args = (_typed(dY, "dY", 2), _typed(X, "X", 2, dY.dtype), _typed(Off, "Off", 1, i32), None if Row is None else _typed(Row, "Row", 1, i32),
             _typed(dW, "dW", 3, None if dW.dtype is torch.float32 else dY.dtype))
@@ -499,6 +528,10 @@ def tc_expert_mm_grad_w(dY, X, Off, Row, dW, workspace=None, add: bool = False, 
 
 def tc_expert_sum(Y, Wt, Place, O, stream=None) -> None:
     """O[T,N] = the sum over i of Wt[T,k] (None: ones) times the rows Place[T,k] of Y[R,N]; a place outside [0, R) takes no part."""
+    if _FAST is not None:
+        status = _FAST.expert_sum(_AT["tc_expert_sum"], Y, Wt, Place, O, stream)
+        if status >= 0:
+            return _check(status, "tc_expert_sum")
     args = (_typed(Y, "Y", 2), None if Wt is None else _typed(Wt, "Wt", 2, torch.float32), _typed(Place, "Place", 2, torch.int32), _typed(O, "O", 2, Y.dtype))
     (R, N), (T, k) = Y.shape, Place.shape
     _fit(tuple(O.shape) == (T, N) and (Wt is None or tuple(Wt.shape) == (T, k)), "tc_expert_sum")
@@ -507,6 +540,10 @@ def tc_expert_sum(Y, Wt, Place, O, stream=None) -> None:
 
 def tc_expert_sum_grad(dO, Y, Wt, Place, dY, dWt, stream=None) -> None:
     """dY[R,N] (rows of the places that occur) and dWt[T,k]: the gradients of tc_expert_sum, from dO[T,N]."""
+    if _FAST is not None:
+        status = _FAST.expert_sum_grad(_AT["tc_expert_sum_grad"], dO, Y, Wt, Place, dY, dWt, stream)
+        if status >= 0:
+            return _check(status, "tc_expert_sum_grad")
     args = (_typed(dO, "dO", 2), _typed(Y, "Y", 2, dO.dtype), _typed(Wt, "Wt", 2, torch.float32), _typed(Place, "Place", 2, torch.int32),
             _typed(dY, "dY", 2, dO.dtype), _typed(dWt, "dWt", 2, torch.float32))
     (R, N), (T, k) = Y.shape, Place.shape
