@@ -99,18 +99,36 @@ __device__ __forceinline__ bool expert_tile(const int* off, int E, int R, int bm
 
 // ---- operands: memory to LDS, LDS to fragments ------------------------------------------------------------------------
 
-// 16 bytes of a row from element `at` on, of which `left` elements are there.
-template <typename T>
-__device__ __forceinline__ u4 emm_load_any(const T* p, int left) {
+// How operands reach LDS: WHOLE, straight from rows of whole 16-byte pieces; ANY, through registers, from rows of any width and alignment;
+// NARROW, the same element by element, where one operand's rows have less than 16 bytes.
+enum { EMM_WHOLE = 0, EMM_ANY = 1, EMM_NARROW = 2 };
+
+// 16 bytes of a row of `width` elements from element `at` on, in two steps: loaded whole from within the row, without a branch, which would make
+// each load wait for the one before; and, when they are needed, shifted to their places with zeros past the row's end.
+template <typename T, int MODE>
+__device__ __forceinline__ u4 emm_load_within(const T* row, int at, int width) {
   constexpr int PER = Elem<T>::PER16;
+  if constexpr (MODE != EMM_NARROW) return __builtin_bit_cast(u4, load_pack<T, PER>(row + min(at, width - PER)));
+  const int a = width >= PER ? min(at, width - PER) : 0;
   Pack<T, PER> v;
-  if (left >= PER) {
-    v = load_pack<T, PER>(p);
-  } else {
 #pragma unroll
-    for (int i = 0; i < PER; i++) v.e[i] = i < left ? p[i] : static_cast<T>(0.0f);
-  }
+  for (int i = 0; i < PER; i++) v.e[i] = a + i < width ? row[a + i] : static_cast<T>(0.0f);
   return __builtin_bit_cast(u4, v);
+}
+template <typename T>
+__device__ __forceinline__ u4 emm_shift(u4 x, int at, int width) {
+  constexpr int PER = Elem<T>::PER16, BITS = 8 * sizeof(T);
+  const int shift = min(at - (width >= PER ? min(at, width - PER) : 0), PER) * BITS;
+  typedef unsigned long long two __attribute__((ext_vector_type(2)));
+  const two v = __builtin_bit_cast(two, x);
+  const unsigned long long down = v[1] >> (shift & 63);
+  const two part = {shift >= 64 ? down : shift ? v[0] >> shift | v[1] << (64 - shift) : v[0], shift >= 64 ? 0 : down};
+  return shift >= 128 ? u4{0, 0, 0, 0} : __builtin_bit_cast(u4, part);
+}
+template <typename T>
+__device__ __forceinline__ u4 emm_load_any(const T* row, int at, int width) {
+  if (width < Elem<T>::PER16) return emm_shift<T>(emm_load_within<T, EMM_NARROW>(row, at, width), at, width);
+  return emm_shift<T>(emm_load_within<T, EMM_ANY>(row, at, width), at, width);
 }
 
 // Operand along its rows: ROWS rows of the tile, 128 bytes of the reduction a stage.  NW wavefronts load it, 8 rows an instruction.
@@ -156,15 +174,19 @@ struct AlongRows {
     }
     next();
   }
+  template <int MODE>
   __device__ __forceinline__ void hold(int, int) {
 #pragma unroll
     for (int j = 0; j < PER; j++) {
-      held[j] = u4{0, 0, 0, 0};
-      if (q0 + at < Q) held[j] = emm_load_any(reinterpret_cast<const T*>(where(j)), Q - q0 - at);
+      held[j] = emm_load_within<T, MODE>(reinterpret_cast<const T*>(where(j)) - (q0 + at), q0 + at, Q);
     }
     next();
   }
-  __device__ __forceinline__ void put(lds_char* lds, int wave, int lane) {
+  __device__ __forceinline__ void put(lds_char* lds, int wave, int lane) {  // (what was fetched last: the stage before q0)
+    if (q0 > Q) {
+#pragma unroll
+      for (int j = 0; j < PER; j++) held[j] = emm_shift<T>(held[j], q0 - BK + at, Q);
+    }
 #pragma unroll
     for (int j = 0; j < PER; j++) *(__attribute__((address_space(3))) u4*)(lds + (wave * PER + j) * 1024 + lane * 16) = held[j];
   }
@@ -199,6 +221,8 @@ struct AcrossRows {
   unsigned off[ANYWHERE ? 1 : PER];
   int src[ANYWHERE ? PER : 1];
   u4 held[PER];
+  unsigned fetched;  // which of them are there
+  bool edge;         // the tile passes the last column
 
   // rows that one instruction reads together have different chunks of 64 banks
   static __device__ __forceinline__ int swizzle(int r) {
@@ -208,7 +232,7 @@ struct AcrossRows {
   }
   static __device__ __forceinline__ int at(int j, int wave, int lane) { return (wave * PER + j) * RPI + lane / CPR; }
 
-  template <bool ANY>
+  template <int MODE>
   __device__ __forceinline__ void begin(const T* b, int64_t stride, const int* rw, int q, int total, int c0, int width, int wave, int lane) {
     base = b;
     row = rw;
@@ -217,10 +241,12 @@ struct AcrossRows {
     Q = q;
     rows = total;
     cols = width;
+    edge = c0 + COLS > width;
+    fetched = 0;
 #pragma unroll
     for (int j = 0; j < PER; j++) {
       col[j] = c0 + ((lane % CPR) ^ swizzle(at(j, wave, lane))) * Elem<T>::PER16;
-      if (!ANY) col[j] = min(col[j], cols - Elem<T>::PER16);
+      if (MODE == EMM_WHOLE) col[j] = min(col[j], cols - Elem<T>::PER16);
       if constexpr (!ANYWHERE) off[j] = (unsigned)(at(j, wave, lane) * ld + col[j]) * (unsigned)sizeof(T);
     }
     if constexpr (ANYWHERE) look(wave, lane);
@@ -255,15 +281,26 @@ struct AcrossRows {
     }
     next(wave, lane);
   }
+  template <int MODE>
   __device__ __forceinline__ void hold(int wave, int lane) {
 #pragma unroll
     for (int j = 0; j < PER; j++) {
-      held[j] = u4{0, 0, 0, 0};
-      if (col[j] < cols && there(j, wave, lane)) held[j] = emm_load_any(where(j), cols - col[j]);
+      const bool in = there(j, wave, lane);  // (a row that is not there: any that is, made zeros when it is put)
+      const T* r = ANYWHERE ? base + (int64_t)(in ? src[ANYWHERE ? j : 0] : 0) * ld : base + (in ? (int64_t)at(j, wave, lane) : (int64_t)-q0) * ld;
+      if (rows > 0) held[j] = emm_load_within<T, MODE>(r, col[j], cols);
+      fetched = (fetched & ~(1u << j)) | (in ? 1u << j : 0);
     }
     next(wave, lane);
   }
   __device__ __forceinline__ void put(lds_char* lds, int wave, int lane) {
+    if (edge) {
+#pragma unroll
+      for (int j = 0; j < PER; j++) held[j] = emm_shift<T>(held[j], col[j], cols);
+    }
+    if (ANYWHERE || q0 > Q) {
+#pragma unroll
+      for (int j = 0; j < PER; j++) held[j] = fetched >> j & 1 ? held[j] : u4{0, 0, 0, 0};
+    }
 #pragma unroll
     for (int j = 0; j < PER; j++) *(__attribute__((address_space(3))) u4*)(lds + (wave * PER + j) * 1024 + lane * 16) = held[j];
   }
@@ -314,18 +351,18 @@ __device__ __forceinline__ f4 emm_mfma(u4 a, u4 b, f4 c) {
 
 // Traffic of half a stage: what goes into buffer `then`, and the fragments of half s that come out of buffer `now`.  (Restricted
 // pointers of a function of their own: the compiler would wait for all loads to LDS before any LDS read that they might concern.)
-template <bool ANY, int MI, int NI, typename A, typename B>
+template <int MODE, int MI, int NI, typename A, typename B>
 __device__ __forceinline__ void emm_traffic(A& a, B& b, const lds_char* __restrict__ now, lds_char* __restrict__ then, int s, bool read, bool more, bool held,
                                             int rm, int cn, int wave, int lane, u4 (&fa)[MI], u4 (&fb)[NI]) {
   const int i = lane & 15, q = lane >> 4;
-  if constexpr (ANY) {
+  if constexpr (MODE != EMM_WHOLE) {
     if (held) {
       a.put(then, wave, lane);
       b.put(then + A::BYTES, wave, lane);
     }
     if (more) {
-      a.hold(wave, lane);
-      b.hold(wave, lane);
+      a.template hold<MODE>(wave, lane);
+      b.template hold<MODE>(wave, lane);
     }
   } else {
     if (more) {
@@ -351,7 +388,7 @@ __device__ __forceinline__ void emm_wait_stages(int stages) {
 }
 
 // MI x NI blocks of 16 x 16 per wavefront, at row rm and column cn of the tile.
-template <typename T, bool ANY, int D, int MI, int NI, typename A, typename B>
+template <typename T, int MODE, int D, int MI, int NI, typename A, typename B>
 __device__ __forceinline__ void emm_loop(A& a, B& b, lds_char* lds, int stages, int rm, int cn, int wave, int lane, f4 (&acc)[MI][NI]) {
   constexpr int STAGE = A::BYTES + B::BYTES, P = A::PER + B::PER;
 #pragma unroll
@@ -360,17 +397,17 @@ __device__ __forceinline__ void emm_loop(A& a, B& b, lds_char* lds, int stages, 
     for (int n = 0; n < NI; n++) acc[m][n] = f4{0, 0, 0, 0};
   if (stages <= 0) return;
   u4 fa[2][MI], fb[2][NI];
-  if constexpr (ANY) {  // stage t + 2 is written, and t + 3 fetched, while the second half of stage t is multiplied
+  if constexpr (MODE != EMM_WHOLE) {  // stage t + 2 is written, and t + 3 fetched, while the second half of stage t is multiplied
     static_assert(D == 2, "buffers");
 #pragma unroll
     for (int j = 0; j < 2; j++) {
-      a.hold(wave, lane);
-      b.hold(wave, lane);
+      a.template hold<MODE>(wave, lane);
+      b.template hold<MODE>(wave, lane);
       a.put(lds + j * STAGE, wave, lane);
       b.put(lds + j * STAGE + A::BYTES, wave, lane);
     }
-    a.hold(wave, lane);
-    b.hold(wave, lane);
+    a.template hold<MODE>(wave, lane);
+    b.template hold<MODE>(wave, lane);
   } else {
 #pragma unroll
     for (int j = 0; j < D; j++)
@@ -383,21 +420,21 @@ __device__ __forceinline__ void emm_loop(A& a, B& b, lds_char* lds, int stages, 
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
-  emm_traffic<ANY, MI, NI>(a, b, lds, lds, 0, true, false, false, rm, cn, wave, lane, fa[0], fb[0]);
+  emm_traffic<MODE, MI, NI>(a, b, lds, lds, 0, true, false, false, rm, cn, wave, lane, fa[0], fb[0]);
   int at = 0;  // buffer of stage t
   for (int t = 0; t < stages; t++) {
     lds_char* const now = lds + at * STAGE;
     at = at + 1 == D ? 0 : at + 1;
-    emm_traffic<ANY, MI, NI>(a, b, now, now, 1, true, false, false, rm, cn, wave, lane, fa[1], fb[1]);
+    emm_traffic<MODE, MI, NI>(a, b, now, now, 1, true, false, false, rm, cn, wave, lane, fa[1], fb[1]);
 #pragma unroll
     for (int m = 0; m < MI; m++)
 #pragma unroll
       for (int n = 0; n < NI; n++) acc[m][n] = emm_mfma<T>(fb[0][n], fa[0][m], acc[m][n]);
-    if constexpr (!ANY) emm_wait_stages<P, D - 2>(stages - 2 - t);
+    if constexpr (MODE == EMM_WHOLE) emm_wait_stages<P, D - 2>(stages - 2 - t);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();  // stage t + 1 is in LDS, and everyone has read stage t
     asm volatile("" ::: "memory");
-    emm_traffic<ANY, MI, NI>(a, b, lds + at * STAGE, now, 0, t + 1 < stages, t + (ANY ? 3 : D) < stages, t + 2 < stages, rm, cn, wave, lane, fa[0], fb[0]);
+    emm_traffic<MODE, MI, NI>(a, b, lds + at * STAGE, now, 0, t + 1 < stages, t + (MODE != EMM_WHOLE ? 3 : D) < stages, t + 2 < stages, rm, cn, wave, lane, fa[0], fb[0]);
 #pragma unroll
     for (int m = 0; m < MI; m++)
 #pragma unroll
@@ -436,7 +473,7 @@ struct ExpertRowsArgs {
 };
 
 // ACROSS: the weights' rows are the reduction (dX), else they are the output's columns (Y).
-template <typename T, bool ACROSS, bool ANY, int BM, int BN, int WM, int WN, int D>
+template <typename T, bool ACROSS, int MODE, int BM, int BN, int WM, int WN, int D>
 __global__ __launch_bounds__(64 * WM * WN) void expert_rows_tile_kernel(ExpertRowsArgs p) {
   constexpr int NW = WM * WN, MI = BM / WM / 16, NI = BN / WN / 16;
   typedef AlongRows<T, BM, NW, true> OpA;
@@ -462,14 +499,14 @@ __global__ __launch_bounds__(64 * WM * WN) void expert_rows_tile_kernel(ExpertRo
     });
     const T* w = static_cast<const T*>(p.W) + (int64_t)e * p.Q * p.NO;
     if constexpr (ACROSS) {
-      b.template begin<ANY>(w, ldw, nullptr, p.Q, p.Q, n0, p.NO, wave, lane);
+      b.template begin<MODE>(w, ldw, nullptr, p.Q, p.Q, n0, p.NO, wave, lane);
     } else {
       const int most = p.NO - 1 - n0;
       b.begin(w + n0 * ldw, ldw, p.Q, wave, lane, [&](int j) -> int64_t { return min(j, most); });
     }
   }
   const int stages = owned ? (p.Q + OpA::BK - 1) / OpA::BK : 0;
-  emm_loop<T, ANY, D, MI, NI>(a, b, (lds_char*)lds, stages, rm, cn, wave, lane, acc);
+  emm_loop<T, MODE, D, MI, NI>(a, b, (lds_char*)lds, stages, rm, cn, wave, lane, acc);
   const int i = lane & 15, q = lane >> 4;
   const bool by4 = (p.NO & 3) == 0;
 #pragma unroll
@@ -516,7 +553,7 @@ struct ExpertWeightsArgs {
   int add;
 };
 
-template <typename T, typename TO, bool ANY, bool LIST, int BM, int BN, int WM, int WN, int D>
+template <typename T, typename TO, int MODE, bool LIST, int BM, int BN, int WM, int WN, int D>
 __global__ __launch_bounds__(64 * WM * WN) void expert_weights_kernel(ExpertWeightsArgs p) {
   constexpr int NW = WM * WN, MI = BM / WM / 16, NI = BN / WN / 16;
   typedef AcrossRows<T, BM, NW, false> OpA;
@@ -534,10 +571,10 @@ __global__ __launch_bounds__(64 * WM * WN) void expert_weights_kernel(ExpertWeig
   f4 acc[MI][NI];
   OpA a;
   OpB b;
-  a.template begin<ANY>(static_cast<const T*>(p.dY) + (int64_t)lo * p.N, p.N, nullptr, rows, rows, m0, p.N, wave, lane);
-  if constexpr (LIST) b.template begin<ANY>(static_cast<const T*>(p.X), p.K, p.row + lo, rows, p.T, n0, p.K, wave, lane);
-  else b.template begin<ANY>(static_cast<const T*>(p.X) + (int64_t)lo * p.K, p.K, nullptr, rows, rows, n0, p.K, wave, lane);
-  emm_loop<T, ANY, D, MI, NI>(a, b, (lds_char*)lds, (rows + OpA::BK - 1) / OpA::BK, rm, cn, wave, lane, acc);
+  a.template begin<MODE>(static_cast<const T*>(p.dY) + (int64_t)lo * p.N, p.N, nullptr, rows, rows, m0, p.N, wave, lane);
+  if constexpr (LIST) b.template begin<MODE>(static_cast<const T*>(p.X), p.K, p.row + lo, rows, p.T, n0, p.K, wave, lane);
+  else b.template begin<MODE>(static_cast<const T*>(p.X) + (int64_t)lo * p.K, p.K, nullptr, rows, rows, n0, p.K, wave, lane);
+  emm_loop<T, MODE, D, MI, NI>(a, b, (lds_char*)lds, (rows + OpA::BK - 1) / OpA::BK, rm, cn, wave, lane, acc);
   const int i = lane & 15, q = lane >> 4;
   const bool by4 = (p.K & 3) == 0;
   TO* out = static_cast<TO*>(p.dW) + (int64_t)e * p.N * p.K;

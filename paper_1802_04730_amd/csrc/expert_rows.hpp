@@ -61,12 +61,12 @@ __global__ __launch_bounds__(64 * WK) void expert_few_rows_kernel(ExpertRowsArgs
       for (int m = 0; m < RT; m++) a[m] += U * STEP;
     }
     for (; s < last; s++) {
-      const int left = p.Q - s * STEP - q * PER;
+      const int at = s * STEP + q * PER;  // (of a pointer that has come this far)
       u4 fb[CT], fa[RT];
 #pragma unroll
-      for (int n = 0; n < CT; n++) fb[n] = left > 0 ? emm_load_any(b[n], left) : u4{0, 0, 0, 0};
+      for (int n = 0; n < CT; n++) fb[n] = emm_load_any(b[n] - at, at, p.Q);
 #pragma unroll
-      for (int m = 0; m < RT; m++) fa[m] = left > 0 ? emm_load_any(a[m], left) : u4{0, 0, 0, 0};
+      for (int m = 0; m < RT; m++) fa[m] = emm_load_any(a[m] - at, at, p.Q);
 #pragma unroll
       for (int m = 0; m < RT; m++)
 #pragma unroll

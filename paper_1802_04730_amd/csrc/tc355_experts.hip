@@ -159,12 +159,12 @@ int64_t route_ws(int64_t T, int64_t E) {
 
 // ---- products grouped by expert -----------------------------------------------------------------------------------------------
 
-template <typename T, bool ACROSS, bool ANY, int BM, int BN, int WM, int WN, int D>
+template <typename T, bool ACROSS, int MODE, int BM, int BN, int WM, int WN, int D>
 tc_status launch_rows_tile(ExpertRowsArgs a, hipStream_t s) {
   a.nt = (int)ceil_div(a.NO, BN);
   const int64_t grid = (most_row_tiles(a.R, a.E, BM) * a.nt + 7) / 8 * 8;
   if (grid > kMostIndex / (64 * WM * WN) * 2) return TC_ERR_UNSUPPORTED;
-  expert_rows_tile_kernel<T, ACROSS, ANY, BM, BN, WM, WN, D><<<dim3((unsigned)grid), dim3(64 * WM * WN), 0, s>>>(a);
+  expert_rows_tile_kernel<T, ACROSS, MODE, BM, BN, WM, WN, D><<<dim3((unsigned)grid), dim3(64 * WM * WN), 0, s>>>(a);
   return launched();
 }
 
@@ -181,40 +181,44 @@ template <bool ACROSS>
 tc_status run_rows(const ExpertRowsArgs& a, tc_type type, hipStream_t s) {
   return by_type(type, [&](auto t) {
     typedef decltype(t) T;
-    const bool whole = (int64_t)a.Q * sizeof(T) % 16 == 0 && (!ACROSS || (int64_t)a.NO * sizeof(T) % 16 == 0);
-    const int most = sizeof(T) == 4 ? 64 : whole && !ACROSS ? 256 : 128;
+    constexpr int PER = Elem<T>::PER16;
+    const bool whole = a.Q % PER == 0 && (!ACROSS || a.NO % PER == 0), thin = a.Q < PER || (ACROSS && a.NO < PER);
+    const int most = sizeof(T) == 4 || thin ? 64 : whole && !ACROSS ? 256 : 128;
     const int side = expert_tile_side(most, compute_units(), [&](int b) { return expected_row_tiles(a.R, a.E, b) * (double)ceil_div(a.NO, b); });
     if constexpr (sizeof(T) == 2) {
       if constexpr (!ACROSS)
-        if (side == 256) return launch_rows_tile<T, ACROSS, false, 256, 256, 2, 4, 2>(a, s);
-      if (side == 128) return whole ? launch_rows_tile<T, ACROSS, false, 128, 128, 2, 4, 2>(a, s) : launch_rows_tile<T, ACROSS, true, 128, 128, 2, 4, 2>(a, s);
+        if (side == 256) return launch_rows_tile<T, ACROSS, EMM_WHOLE, 256, 256, 2, 4, 2>(a, s);
+      if (side == 128) return whole ? launch_rows_tile<T, ACROSS, EMM_WHOLE, 128, 128, 2, 4, 2>(a, s) : launch_rows_tile<T, ACROSS, EMM_ANY, 128, 128, 2, 4, 2>(a, s);
     }
-    return whole ? launch_rows_tile<T, ACROSS, false, 64, 64, 2, 2, 3>(a, s) : launch_rows_tile<T, ACROSS, true, 64, 64, 2, 2, 2>(a, s);
+    if (thin) return launch_rows_tile<T, ACROSS, EMM_NARROW, 64, 64, 2, 2, 2>(a, s);
+    return whole ? launch_rows_tile<T, ACROSS, EMM_WHOLE, 64, 64, 2, 2, 2>(a, s) : launch_rows_tile<T, ACROSS, EMM_ANY, 64, 64, 2, 2, 2>(a, s);
   });
 }
 
-template <typename T, typename TO, bool ANY, bool LIST, int BM, int BN, int WM, int WN, int D>
+template <typename T, typename TO, int MODE, bool LIST, int BM, int BN, int WM, int WN, int D>
 tc_status launch_weights_list(ExpertWeightsArgs a, hipStream_t s) {
   a.mt = (int)ceil_div(a.N, BM);
   a.nt = (int)ceil_div(a.K, BN);
   const int64_t share = ceil_div((int64_t)a.mt * a.nt, 8);
   if (prod_reaches({share, 8, a.E}, kMostIndex / (64 * WM * WN) * 2)) return TC_ERR_UNSUPPORTED;
   const int64_t grid = 8 * share * a.E;
-  expert_weights_kernel<T, TO, ANY, LIST, BM, BN, WM, WN, D><<<dim3((unsigned)grid), dim3(64 * WM * WN), 0, s>>>(a);
+  expert_weights_kernel<T, TO, MODE, LIST, BM, BN, WM, WN, D><<<dim3((unsigned)grid), dim3(64 * WM * WN), 0, s>>>(a);
   return launched();
 }
-template <typename T, typename TO, bool ANY, int B, int WM, int WN, int D>
+template <typename T, typename TO, int MODE, int B, int WM, int WN, int D>
 tc_status launch_weights(const ExpertWeightsArgs& a, hipStream_t s) {
-  return a.row ? launch_weights_list<T, TO, ANY, true, B, B, WM, WN, D>(a, s) : launch_weights_list<T, TO, ANY, false, B, B, WM, WN, D>(a, s);
+  return a.row ? launch_weights_list<T, TO, MODE, true, B, B, WM, WN, D>(a, s) : launch_weights_list<T, TO, MODE, false, B, B, WM, WN, D>(a, s);
 }
 template <typename T, typename TO>
 tc_status run_weights(const ExpertWeightsArgs& a, hipStream_t s) {
-  const bool whole = (int64_t)a.N * sizeof(T) % 16 == 0 && (int64_t)a.K * sizeof(T) % 16 == 0;
-  const int side = expert_tile_side(sizeof(T) == 4 ? 64 : 128, compute_units(),
+  constexpr int PER = Elem<T>::PER16;
+  const bool whole = a.N % PER == 0 && a.K % PER == 0, thin = a.N < PER || a.K < PER;
+  const int side = expert_tile_side(sizeof(T) == 4 || thin ? 64 : 128, compute_units(),
                                     [&](int b) { return (double)a.E * (double)ceil_div(a.N, b) * (double)ceil_div(a.K, b); });
   if constexpr (sizeof(T) == 2)
-    if (side == 128) return whole ? launch_weights<T, TO, false, 128, 2, 4, 2>(a, s) : launch_weights<T, TO, true, 128, 2, 4, 2>(a, s);
-  return whole ? launch_weights<T, TO, false, 64, 2, 2, 3>(a, s) : launch_weights<T, TO, true, 64, 2, 2, 2>(a, s);
+    if (side == 128) return whole ? launch_weights<T, TO, EMM_WHOLE, 128, 2, 4, 2>(a, s) : launch_weights<T, TO, EMM_ANY, 128, 2, 4, 2>(a, s);
+  if (thin) return launch_weights<T, TO, EMM_NARROW, 64, 2, 2, 2>(a, s);
+  return whole ? launch_weights<T, TO, EMM_WHOLE, 64, 2, 2, 2>(a, s) : launch_weights<T, TO, EMM_ANY, 64, 2, 2, 2>(a, s);
 }
 
 }  // namespace
