@@ -476,7 +476,8 @@ struct ExpertRowsArgs {
 template <typename T, bool ACROSS, int MODE, int BM, int BN, int WM, int WN, int D>
 __global__ __launch_bounds__(64 * WM * WN) void expert_rows_tile_kernel(ExpertRowsArgs p) {
   constexpr int NW = WM * WN, MI = BM / WM / 16, NI = BN / WN / 16;
-  typedef AlongRows<T, BM, NW, true> OpA;
+  // (a tile of 256 has no registers left for addresses anywhere: the host sees to it that its rows lie within 4 GB)
+  typedef AlongRows<T, BM, NW, BM != 256> OpA;
   typedef std::conditional_t<ACROSS, AcrossRows<T, BN, NW, false>, AlongRows<T, BN, NW, false>> OpB;
   __shared__ __align__(16) char lds[D * (OpA::BYTES + OpB::BYTES)];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);

@@ -17,7 +17,7 @@ inline double expected_row_tiles(int64_t R, int64_t E, int64_t bm) { return (dou
 // tile's products, over the rate that the side reaches on large extents (relative to 256; 16-bit storage, 8192^3: 1268, 1092 TFLOP/s
 // and about 780).  Larger tiles read less per product; smaller ones lose less to the last row tile of an expert and to compute units
 // without a tile.  Measured, us, sides 256 / 128 / 64: (E,R,N,K) = (8,16384,4096,4096) 492 / 617 / -, (16,8192,4096,2048) 195 / 192 / 266,
-// (16,2048,2048,2048) 51 / 36 / 41, (4,2000,512,512) 21 / 12 / 10.  fp32 takes 64 always: at a rate of the matrix core that is a sixteenth, no tile is
+// (16,2048,2048,2048) 51 / 36 / 41, (4,2000,512,512) 21 / 12 / 8.  fp32 takes 64 always: at a rate of the matrix core that is a sixteenth, no tile is
 // short of operands ((16,2048,2048,2048) 497 / 259 / 223, (64,16384,1024,2048) 1023 / 777 / 692); products with an operand across its rows
 // take 128 at most, since 256 has too few registers left for them (dX and dW of (8,16384,4096,4096): 557 and 856 / 613 and 618).
 template <typename F>

@@ -183,7 +183,8 @@ tc_status run_rows(const ExpertRowsArgs& a, tc_type type, hipStream_t s) {
     typedef decltype(t) T;
     constexpr int PER = Elem<T>::PER16;
     const bool whole = a.Q % PER == 0 && (!ACROSS || a.NO % PER == 0), thin = a.Q < PER || (ACROSS && a.NO < PER);
-    const int most = sizeof(T) == 4 || thin ? 64 : whole && !ACROSS ? 256 : 128;
+    const bool near = !prod_reaches({std::max(a.T, 1), a.Q, (int64_t)sizeof(T)}, (int64_t)1 << 32);
+    const int most = sizeof(T) == 4 || thin ? 64 : whole && near && !ACROSS ? 256 : 128;
     const int side = expert_tile_side(most, compute_units(), [&](int b) { return expected_row_tiles(a.R, a.E, b) * (double)ceil_div(a.NO, b); });
     if constexpr (sizeof(T) == 2) {
       if constexpr (!ACROSS)
