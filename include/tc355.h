@@ -110,7 +110,8 @@ int64_t tc355_get_option(tc_option key);
  *   embed_grad: small_sort, sort
  *   route:  one, tiles
  *   expert_mm: rows (experts with few rows), tile
- *   expert_mm_grad_x, expert_mm_grad_w: tile
+ *   expert_mm_grad_x: tile
+ *   expert_mm_grad_w: tile, parts (tiles of parts of the rows, joined)
  * A debugging and testing aid: tests pick the tolerance of the
  * arithmetic that actually ran instead of re-deriving the dispatch.
  */
@@ -525,7 +526,9 @@ tc_status tc_expert_mm_grad_x(const void *dY, const void *W,
  * dW: [E,N,K], of dY's type or fp32 (grad_type); add = 1 adds to what it holds,
  * add = 0 writes all of it, zeros for an expert without rows.
  *   workspace  as in tc_tbmm_ws: device scratch of tc_expert_mm_grad_w_workspace_bytes(...)
- *              bytes, 16-byte aligned; NULL or fewer bytes only cost time.
+ *              bytes (of the current device), 16-byte aligned; NULL or fewer bytes only cost
+ *              time: with it, long experts' rows are cut into parts whose sums are joined
+ *              in order where the weights alone have few tiles.
  */
 size_t tc_expert_mm_grad_w_workspace_bytes(int64_t R, int64_t E, int64_t N,
                                            int64_t K);

@@ -543,6 +543,8 @@ __global__ __launch_bounds__(64 * WM * WN) void expert_rows_tile_kernel(ExpertRo
   }
 }
 
+// With parts, blockIdx.y takes its share of the expert's rows (whole stages but for the last part's end) and dW is the workspace,
+// [parts][E][N][K] of fp32, which expert_weights_join_kernel adds up in the parts' order.
 struct ExpertWeightsArgs {
   const void* dY;  // [R][N]
   const void* X;   // [T][K], taken through `row`, or [R][K]
@@ -551,7 +553,7 @@ struct ExpertWeightsArgs {
   const int* row;
   int R, T, E, N, K;
   int nt, mt;  // tiles of K, of N
-  int add;
+  int add, parts;
 };
 
 template <typename T, typename TO, int MODE, bool LIST, int BM, int BN, int WM, int WN, int D>
@@ -567,7 +569,14 @@ __global__ __launch_bounds__(64 * WM * WN) void expert_weights_kernel(ExpertWeig
   if (e >= p.E || in >= per) return;
   const int block = in / (8 * p.nt), rest = in % (8 * p.nt), height = min(8, p.mt - 8 * block);
   const int m0 = (8 * block + rest % height) * BM, n0 = (rest / height) * BN;
-  const int lo = min(max(p.off[e], 0), p.R), hi = min(max(p.off[e + 1], 0), p.R), rows = max(hi - lo, 0);
+  int lo = min(max(p.off[e], 0), p.R), hi = min(max(p.off[e + 1], 0), p.R);
+  if (p.parts > 1) {
+    constexpr int BK = OpA::BK;
+    const int share = (max(hi - lo, 0) + p.parts * BK - 1) / (p.parts * BK) * BK;
+    hi = (int)min((int64_t)hi, lo + (int64_t)(blockIdx.y + 1) * share);
+    lo = (int)min((int64_t)max(hi, lo), lo + (int64_t)blockIdx.y * share);
+  }
+  const int rows = max(hi - lo, 0);
   const int rm = (wave / WN) * (BM / WM), cn = (wave % WN) * (BN / WN);
   f4 acc[MI][NI];
   OpA a;
@@ -578,7 +587,7 @@ __global__ __launch_bounds__(64 * WM * WN) void expert_weights_kernel(ExpertWeig
   emm_loop<T, MODE, D, MI, NI>(a, b, (lds_char*)lds, (rows + OpA::BK - 1) / OpA::BK, rm, cn, wave, lane, acc);
   const int i = lane & 15, q = lane >> 4;
   const bool by4 = (p.K & 3) == 0;
-  TO* out = static_cast<TO*>(p.dW) + (int64_t)e * p.N * p.K;
+  TO* out = static_cast<TO*>(p.dW) + ((int64_t)blockIdx.y * p.E + e) * p.N * p.K;
 #pragma unroll
   for (int m = 0; m < MI; m++) {
     const int r = m0 + rm + 16 * m + i;
@@ -597,6 +606,26 @@ __global__ __launch_bounds__(64 * WM * WN) void expert_weights_kernel(ExpertWeig
       emm_store(o, p.K - c, by4, v);
     }
   }
+}
+
+// dW (+)= the sum of the parts, four neighbours a thread.
+template <typename TO>
+__global__ __launch_bounds__(WG_THREADS) void expert_weights_join_kernel(const float* part, void* dW, int64_t n, int parts, int add) {
+  const int64_t at = ((int64_t)blockIdx.x * WG_THREADS + threadIdx.x) * 4;
+  if (at >= n) return;
+  const int left = (int)min((int64_t)4, n - at);
+  f4 v = {0, 0, 0, 0};
+  for (int s = 0; s < parts; s++)
+#pragma unroll
+    for (int x = 0; x < 4; x++)
+      if (x < left) v[x] += part[s * n + at + x];
+  TO* o = static_cast<TO*>(dW) + at;
+  if (add) {
+#pragma unroll
+    for (int x = 0; x < 4; x++)
+      if (x < left) v[x] += static_cast<float>(o[x]);
+  }
+  emm_store(o, left, left == 4, v);
 }
 
 }  // namespace tc355

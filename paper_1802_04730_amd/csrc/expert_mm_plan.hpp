@@ -1,5 +1,7 @@
 // Which tile a product grouped by expert takes: host side, from extents and the device (tests compile it by itself).
 #pragma once
+#include <cmath>
+
 #include "tc355_host.hpp"
 
 namespace tc355 {
@@ -33,6 +35,27 @@ int expert_tile_side(int most, int cus, F tiles) {
     const double load = tiles(s.side) / cus, t = (load < 1 ? 1 : load) * s.side * s.side / s.rate;
     if (!best || t < least) {
       best = s.side;
+      least = t;
+    }
+  }
+  return best;
+}
+
+// Parts into which the gradient of the weights cuts each expert's rows: tiles of the weights alone may be too few for the device, and
+// the longest expert's rows take their time however many compute units wait.  Estimated, us: rounds of workgroups (two on a compute unit) times
+// the rows of a part of the longest expert, taken as twice the average, plus, with parts, a launch and the way of the partial sums
+// to the workspace and back; more parts where they save 15 %.  Measured, us, one part / chosen: bfloat16 (E,R,N,K) = (4,65536,256,256)
+// 164 / 40 (8 parts), (1,8192,512,512) 63 / 21 (8); fp32 (4,65536,256,256) 514 / 125 (8), (2,3000,64,64) 42 / 17 (16).
+constexpr int EMM_MOST_PARTS = 16;
+inline int expert_weights_parts(bool f32, int cus, int64_t R, int64_t E, int64_t N, int64_t K, int side) {
+  const double tiles = (double)E * ceil_div(N, side) * ceil_div(K, side), rows = (double)R / E * (E > 1 ? 2 : 1);
+  const double row = side == 128 ? 0.6 / 64 : f32 ? 0.8 / 32 : 0.25 / 64;  // of a tile, us
+  int best = 1;
+  double least = 0;
+  for (int s = 1; s <= EMM_MOST_PARTS; s *= 2) {
+    const double t = std::ceil(tiles * s / (2 * cus)) * (rows / s * row + 3) + (s > 1 ? 5 + 8.0 * s * E * N * K / 4e6 : 0);
+    if (s == 1 || t < 0.85 * least) {
+      best = s;
       least = t;
     }
   }

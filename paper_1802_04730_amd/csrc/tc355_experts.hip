@@ -196,6 +196,16 @@ tc_status run_rows(const ExpertRowsArgs& a, tc_type type, hipStream_t s) {
   });
 }
 
+// The tile's side for the gradient of the weights.
+int weights_side(bool f32, int64_t E, int64_t N, int64_t K) {
+  const int per = f32 ? 4 : 8;
+  return expert_tile_side(f32 || N < per || K < per ? 64 : 128, compute_units(), [&](int b) { return (double)E * (double)ceil_div(N, b) * (double)ceil_div(K, b); });
+}
+int64_t weights_ws(bool f32, int64_t R, int64_t E, int64_t N, int64_t K, int* parts) {
+  *parts = R ? expert_weights_parts(f32, compute_units(), R, E, N, K, weights_side(f32, E, N, K)) : 1;
+  return *parts > 1 ? *parts * E * N * K * 4 : 0;
+}
+
 template <typename T, typename TO, int MODE, bool LIST, int BM, int BN, int WM, int WN, int D>
 tc_status launch_weights_list(ExpertWeightsArgs a, hipStream_t s) {
   a.mt = (int)ceil_div(a.N, BM);
@@ -203,7 +213,7 @@ tc_status launch_weights_list(ExpertWeightsArgs a, hipStream_t s) {
   const int64_t share = ceil_div((int64_t)a.mt * a.nt, 8);
   if (prod_reaches({share, 8, a.E}, kMostIndex / (64 * WM * WN) * 2)) return TC_ERR_UNSUPPORTED;
   const int64_t grid = 8 * share * a.E;
-  expert_weights_kernel<T, TO, MODE, LIST, BM, BN, WM, WN, D><<<dim3((unsigned)grid), dim3(64 * WM * WN), 0, s>>>(a);
+  expert_weights_kernel<T, TO, MODE, LIST, BM, BN, WM, WN, D><<<dim3((unsigned)grid, (unsigned)a.parts), dim3(64 * WM * WN), 0, s>>>(a);
   return launched();
 }
 template <typename T, typename TO, int MODE, int B, int WM, int WN, int D>
@@ -214,8 +224,7 @@ template <typename T, typename TO>
 tc_status run_weights(const ExpertWeightsArgs& a, hipStream_t s) {
   constexpr int PER = Elem<T>::PER16;
   const bool whole = a.N % PER == 0 && a.K % PER == 0, thin = a.N < PER || a.K < PER;
-  const int side = expert_tile_side(sizeof(T) == 4 || thin ? 64 : 128, compute_units(),
-                                    [&](int b) { return (double)a.E * (double)ceil_div(a.N, b) * (double)ceil_div(a.K, b); });
+  const int side = weights_side(sizeof(T) == 4, a.E, a.N, a.K);
   if constexpr (sizeof(T) == 2)
     if (side == 128) return whole ? launch_weights<T, TO, EMM_WHOLE, 128, 2, 4, 2>(a, s) : launch_weights<T, TO, EMM_ANY, 128, 2, 4, 2>(a, s);
   if (thin) return launch_weights<T, TO, EMM_NARROW, 64, 2, 2, 2>(a, s);
@@ -392,13 +401,13 @@ tc_status tc_expert_mm_grad_x(const void* dY, const void* W, const int32_t* Off,
 }
 
 size_t tc_expert_mm_grad_w_workspace_bytes(int64_t R, int64_t E, int64_t N, int64_t K) {
-  (void)R; (void)E; (void)N; (void)K;
-  return 0;
+  if (R <= 0 || E <= 0 || N <= 0 || K <= 0 || R >= kMostRows || E >= kMostRows || N >= kMostWidth || K >= kMostWidth || prod_reaches({E, N, K}, (int64_t)1 << 50)) return 0;
+  int parts;
+  return (size_t)std::max(weights_ws(true, R, E, N, K, &parts), weights_ws(false, R, E, N, K, &parts));
 }
 
 tc_status tc_expert_mm_grad_w(const void* dY, const void* X, const int32_t* Off, const int32_t* Row, void* dW, int64_t T, int64_t R, int64_t E, int64_t N,
                               int64_t K, int32_t add, tc_type type, tc_type grad_type, void* workspace, size_t workspace_bytes, void* hip_stream) {
-  (void)workspace_bytes;
   if (!known(type) || (grad_type != type && grad_type != TC_F32) || T < 0 || R < 0 || E <= 0 || N <= 0 || K <= 0 || (!Row && T != R)) return TC_ERR_SHAPE;
   if (!Off || !dW || (R && (!dY || (T && !X)))) return TC_ERR_NULL;
   if (dW == dY || dW == X || dW == static_cast<const void*>(Off) || dW == static_cast<const void*>(Row)) return TC_ERR_ALIAS;
@@ -406,13 +415,28 @@ tc_status tc_expert_mm_grad_w(const void* dY, const void* X, const int32_t* Off,
     return TC_ERR_ALIAS;
   if (misaligned(dY) || misaligned(X) || misaligned(Off) || misaligned(Row) || misaligned(dW) || misaligned(workspace)) return TC_ERR_ALIGN;
   if (T >= kMostRows || R >= kMostRows || E >= kMostRows || N >= kMostWidth || K >= kMostWidth) return TC_ERR_UNSUPPORTED;
+  if (prod_reaches({E, N, K}, (int64_t)1 << 50)) return TC_ERR_UNSUPPORTED;
   if (R == 0 && add) return TC_OK;
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
-  ExpertWeightsArgs a{dY, X, dW, Off, Row, (int)R, (int)T, (int)E, (int)N, (int)K, 0, 0, add != 0};
-  return took("expert_mm_grad_w:tile", by_type(type, [&](auto t) {
-                typedef decltype(t) T_;
-                return grad_type == TC_F32 ? run_weights<T_, float>(a, s) : run_weights<T_, T_>(a, s);
-              }));
+  ExpertWeightsArgs a{dY, X, dW, Off, Row, (int)R, (int)T, (int)E, (int)N, (int)K, 0, 0, add != 0, 1};
+  int parts;
+  const int64_t need = weights_ws(type == TC_F32, R, E, N, K, &parts);
+  return by_type(type, [&](auto t) {
+    typedef decltype(t) T_;
+    const auto join_to = [&](auto o) {
+      a.dW = workspace;
+      a.parts = parts;
+      a.add = 0;
+      const tc_status st = run_weights<T_, float>(a, s);
+      if (st != TC_OK) return st;
+      const int64_t n = E * N * K, grid = ceil_div(n, 4 * WG_THREADS);
+      expert_weights_join_kernel<decltype(o)><<<dim3((unsigned)grid), dim3(WG_THREADS), 0, s>>>(static_cast<const float*>(workspace), dW, n, parts, add != 0);
+      return took("expert_mm_grad_w:parts", launched());
+    };
+    if (need && workspace && workspace_bytes >= (size_t)need && ceil_div(E * N * K, 4 * WG_THREADS) <= kMostIndex / WG_THREADS * 2)
+      return grad_type == TC_F32 ? join_to(float{}) : join_to(t);
+    return took("expert_mm_grad_w:tile", grad_type == TC_F32 ? run_weights<T_, float>(a, s) : run_weights<T_, T_>(a, s));
+  });
 }
 
 tc_status tc_expert_sum(const void* Y, const float* Wt, const int32_t* Place, void* O, int64_t T, int64_t R, int64_t k, int64_t N, tc_type type,
