@@ -41,7 +41,7 @@ def test_the_large_tiles_are_taken(plans):
 
 def test_small_shapes_take_every_small_kernel(plans):
     kinds = set()
-    for T, R, E, N, K in small.MM_SHAPES:
+    for T, R, E, N, K in small.MM_SHAPES + big.SOME_ROWS:
         kinds.add("few" if R // E < 16 else "some" if R // E < 64 else "tile of %d" % plans.rows_side(256, CUS, R, E, N))
         kinds.add("weights by %d" % plans.weights_side(128, CUS, E, N, K))
         kinds.add("rows' gradient by %d" % plans.rows_side(128, CUS, R, E, K))

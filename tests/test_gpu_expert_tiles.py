@@ -12,6 +12,8 @@ pytestmark = pytest.mark.gpu
 
 # T, R, E, N, K: tiles of 256 forward (of 128 where K is odd), reductions of one stage, of whole ones, of a part of one
 FORWARD = [(1500, 4100, 3, 3600, 200), (700, 4200, 2, 3700, 64), (4000, 4000, 1, 4096, 1000), (900, 5000, 7, 3400, 8), (1000, 4100, 3, 3601, 201)]
+# T, R, E, N, K: some dozens of rows an expert
+SOME_ROWS = [(100, 120, 4, 100, 136), (200, 130, 2, 33, 77), (64, 250, 5, 64, 512), (50, 20, 1, 17, 3), (300, 700, 12, 130, 1000)]
 # R, E, N, K: tiles of 128 for dX
 BACK_X = [(4100, 3, 200, 3600), (4000, 2, 64, 3700), (4100, 5, 1000, 3400), (4100, 3, 201, 3603)]
 # T, R, E, N, K: tiles of 128 for dW
@@ -58,6 +60,20 @@ def test_forward(dtype, T, R, E, N, K):
     x, w = _source(X, Row), W.double()
     want, mag = _by_expert(off, R, N, lambda e, a, b: ((x[a:b] @ w[e].t()).clamp(min=0), x[a:b].abs() @ w[e].abs().t()))
     _close(Y, want, mag, K, dtype)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("T,R,E,N,K", SOME_ROWS)
+@pytest.mark.parametrize("gather", [False, True])
+def test_some_rows_an_expert(dtype, T, R, E, N, K, gather):
+    off = _offsets(R, E, R + 4)
+    Row = _ints(np.random.default_rng(R).integers(-1, T + 1, R)) if gather else None
+    X, W, Y = _rand((T if gather else R, K), dtype, 1), _rand((E, N, K), dtype, 2, K ** -0.5), torch.full((R, N), float("nan"), dtype=dtype, device="cuda")
+    tc.tc_expert_mm(X, W, _ints(off), Row, Y, gather)
+    assert tc.last_path() == "expert_mm:rows"
+    x, w = _source(X, Row), W.double()
+    want, mag = _by_expert(off, R, N, lambda e, a, b: (x[a:b] @ w[e].t(), x[a:b].abs() @ w[e].abs().t()))
+    _close(Y, want.clamp(min=0) if gather else want, mag, K, dtype)
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
