@@ -107,7 +107,7 @@ int64_t tc355_get_option(tc_option key);
  *   sconv:  i8, tile, split
  *   lut:    sum
  *   embed, expert_sum, expert_sum_grad, route_grad: rows
- *   embed_grad: small_sort, sort
+ *   embed_grad: ranks (few tokens), sort
  *   route:  one, tiles
  *   expert_mm: rows (experts with few rows), tile
  *   expert_mm_grad_x: tile

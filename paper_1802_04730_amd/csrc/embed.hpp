@@ -9,7 +9,7 @@
 // inside a chunk go to the table; the ends that a chunk shares with its neighbours go to a workspace, and a second launch joins them, chunk by
 // chunk: language has words that make up a large part of a batch.  No atomics, one order for every sum.  Rows of numbers that do not occur are
 // written with zeros by workgroups of their own in the same launch, or left alone where the gradient is added to what is there.
-// (A group of lanes per row of the table, empty or not: 402 us against EMBED_TRAIN at 32768 tokens of 2048, a table of 131072 rows: three
+// (A group of lanes per row of the table, empty or not: 402 us against 243 and 10 at 32768 tokens of 2048 bfloat16, a table of 131072 rows in fp32: three
 // dependent trips to memory a row.)
 #pragma once
 #include "expert_types.hpp"

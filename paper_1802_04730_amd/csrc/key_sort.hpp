@@ -5,8 +5,7 @@
 // No atomics on memory: the order, and with it every sum taken along it, is the same each time.
 //
 // Lanes of one digit find each other by a ballot per bit of the digit.  Bounded by the latency of a pass's launches at the sizes of a
-// training step (32768 keys of 18 bits: two passes of two launches, SORT_TIME_LARGE); up to SORT_SMALL keys everything stays in one workgroup's LDS, in
-// one launch (1500 keys of 14 bits: SORT_TIME_SMALL).
+// training step (32768 keys of 18 bits: two passes of a count of 4.7 us and a placement of 9.7).  Up to SORT_SMALL keys are ranked by counting instead.
 #pragma once
 #include "tc355_device.hpp"
 
@@ -17,9 +16,9 @@ constexpr int SORT_MOST_BINS = 1 << SORT_MOST_BITS;
 constexpr int SORT_THREADS = 512;
 constexpr int SORT_TILE = 2048;             // keys of a workgroup
 constexpr int SORT_ROUNDS = 4;              // keys of a thread
-constexpr int SORT_SMALL = 4096;            // keys that one workgroup sorts by itself
+constexpr int SORT_SMALL = 8192;            // keys that are ranked by counting
 constexpr int SORT_DIRECT_TILES = 32;       // up to so many workgroups add the earlier ones' counts up themselves
-static_assert(SORT_TILE == SORT_ROUNDS * SORT_THREADS && SORT_SMALL == SORT_ROUNDS * 1024, "keys of a workgroup");
+static_assert(SORT_TILE == SORT_ROUNDS * SORT_THREADS, "keys of a workgroup");
 
 // Lanes of the wavefront that have the same digit (of `bits` bits) as this one, among `on`.
 __device__ __forceinline__ unsigned long long same_digit(int d, int bits, bool on) {
@@ -81,10 +80,10 @@ struct SortPass {
   int summed;       // count holds sums over the earlier tiles; behind the last one, all tiles' sum
 };
 
+__device__ __forceinline__ int row_key(const SortPass& p, int k) { return k < 0 || k >= p.E || k == p.pad ? p.E : k; }
 __device__ __forceinline__ int sort_key(const SortPass& p, int i) {
   const int k = p.key[i];
-  if (p.order) return k;
-  return k < 0 || k >= p.E || k == p.pad ? p.E : k;
+  return p.order ? k : row_key(p, k);
 }
 
 static __global__ __launch_bounds__(SORT_THREADS) void sort_count_kernel(SortPass p) {
@@ -180,65 +179,48 @@ static __global__ __launch_bounds__(SORT_THREADS) void sort_scatter_kernel(SortP
   }
 }
 
-// All digits in one workgroup, n <= SORT_ROUNDS * THREADS.
-template <int THREADS>
-__global__ __launch_bounds__(THREADS) void sort_small_kernel(SortPass p, int key_bits) {
-  constexpr int WAVES = THREADS / 64, ROUNDS = SORT_ROUNDS, MOST = ROUNDS * THREADS;
-  extern __shared__ int mem[];  // keys, indices: MOST each; counters: WAVES * bins; starts: bins
-  __shared__ int part[WAVES];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, bins = 1 << p.bits;
-  int *keys = mem, *idx = mem + MOST, *count = mem + 2 * MOST, *start = count + WAVES * bins;
-  const int first = wave * (MOST / WAVES) + lane;
-  int key[ROUNDS], at[ROUNDS];
+// Few keys, n <= SORT_SMALL: every key's rank is counted among all of them, from LDS; a workgroup ranks 32, eight groups of 32 lanes
+// sharing the list.  n^2 comparisons, but one launch of one round trip to memory: 1500 keys in 5.8 us (all passes in one workgroup's LDS:
+// 8.5), and at 8192 the time of the passes (the whole gradient of 333 columns, 35.0 us at 8192, 35.4 at 8193).
+static __global__ __launch_bounds__(WG_THREADS) void sort_rank_kernel(SortPass p) {
+  constexpr int KEYS = 32, SHARES = WG_THREADS / KEYS;
+  extern __shared__ __align__(16) int keys[];  // n, rounded up to a multiple of 32
+  __shared__ int part[SHARES][KEYS];
+  const int all = (p.n + 31) / 32 * 32, share = all / SHARES;  // (a multiple of 4)
+  for (int j0 = threadIdx.x; j0 < all; j0 += 8 * WG_THREADS) {  // eight loads in flight
+    int k[8];
 #pragma unroll
-  for (int j = 0; j < ROUNDS; j++) {
-    at[j] = first + 64 * j;
-    key[j] = at[j] < p.n ? sort_key(p, at[j]) : 0;
-  }
-  for (int shift = 0; shift < key_bits; shift += p.bits) {
-    for (int b = threadIdx.x; b < WAVES * bins; b += THREADS) count[b] = 0;
-    __syncthreads();
-    int rank[ROUNDS];
+    for (int x = 0; x < 8; x++) k[x] = p.key[min(j0 + x * WG_THREADS, p.n - 1)];
 #pragma unroll
-    for (int j = 0; j < ROUNDS; j++) rank[j] = rank_and_count(count + wave * bins, (key[j] >> shift) & (bins - 1), p.bits, first + 64 * j < p.n, lane);
-    __syncthreads();
-    int run = 0;
-    for (int b0 = 0; b0 < bins; b0 += THREADS) {
-      const int b = b0 + (int)threadIdx.x;
-      int c[WAVES], all = 0, sum;
-#pragma unroll
-      for (int w = 0; w < WAVES; w++) c[w] = b < bins ? count[w * bins + b] : 0;
-#pragma unroll
-      for (int w = 0; w < WAVES; w++) {
-        if (b < bins) count[w * bins + b] = all;
-        all += c[w];
-      }
-      const int lower = block_prefix<WAVES>(all, part, &sum);
-      if (b < bins) start[b] = run + lower;
-      run += sum;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int j = 0; j < ROUNDS; j++) {
-      if (first + 64 * j >= p.n) break;
-      const int d = (key[j] >> shift) & (bins - 1), to = start[d] + count[wave * bins + d] + rank[j];
-      keys[to] = key[j];
-      idx[to] = at[j];
-    }
-    __syncthreads();
-#pragma unroll
-    for (int j = 0; j < ROUNDS; j++) {
-      if (first + 64 * j >= p.n) break;
-      key[j] = keys[first + 64 * j];
-      at[j] = idx[first + 64 * j];
+    for (int x = 0; x < 8; x++) {
+      const int j = j0 + x * WG_THREADS;
+      if (j < all) keys[j] = j < p.n ? row_key(p, k[x]) : 0x7fffffff;  // (above every key)
     }
   }
+  __syncthreads();
+  const int i = blockIdx.x * KEYS + (threadIdx.x & (KEYS - 1)), s = threadIdx.x / KEYS;
+  const int key = keys[i];
+  int rank = 0;
+  typedef int i4 __attribute__((ext_vector_type(4)));
+  for (int j0 = s * share; j0 < (s + 1) * share; j0 += 32) {  // eight reads in flight
+    i4 k[8];
 #pragma unroll
-  for (int j = 0; j < ROUNDS; j++) {
-    if (first + 64 * j >= p.n) break;
-    p.key_out[first + 64 * j] = key[j];
-    p.order_out[first + 64 * j] = at[j];
+    for (int y = 0; y < 8; y++) k[y] = *reinterpret_cast<const i4*>(keys + min(j0 + 4 * y, all - 4));
+#pragma unroll
+    for (int y = 0; y < 8; y++) {
+      const int j = j0 + 4 * y;
+      int more = 0;
+#pragma unroll
+      for (int x = 0; x < 4; x++) more += k[y][x] < key + (j + x < i) ? 1 : 0;  // (an equal one counts if it comes before)
+      rank += j < (s + 1) * share ? more : 0;
+    }
   }
+  part[s][threadIdx.x & (KEYS - 1)] = rank;
+  __syncthreads();
+  if (s || i >= p.n) return;
+  for (int w = 1; w < SHARES; w++) rank += part[w][threadIdx.x];
+  p.key_out[rank] = key;
+  p.order_out[rank] = i;
 }
 
 }  // namespace tc355

@@ -107,10 +107,7 @@ tc_status sort_tokens(const EmbedGradPlan& pl, const int32_t* Idx, int64_t T, in
   if (T <= SORT_SMALL) {
     a.key_out = keys[0];
     a.order_out = orders[0];
-    const auto lds = [&](int threads) { return (2 * (size_t)SORT_ROUNDS * threads + (threads / 64 + 1) * ((size_t)1 << pl.bits)) * 4; };
-    if (T <= SORT_ROUNDS * 256) sort_small_kernel<256><<<1, 256, lds(256), s>>>(a, pl.key_bits);
-    else if (T <= SORT_ROUNDS * 512) sort_small_kernel<512><<<1, 512, lds(512), s>>>(a, pl.key_bits);
-    else sort_small_kernel<1024><<<1, 1024, lds(1024), s>>>(a, pl.key_bits);
+    sort_rank_kernel<<<(unsigned)ceil_div(T, 32), WG_THREADS, (size_t)ceil_div(T, 32) * 32 * 4, s>>>(a);
     *key = keys[0];
     *order = orders[0];
     return launched();
@@ -302,7 +299,7 @@ tc_status tc_embed_grad(const void* dO, const int32_t* Idx, void* dLUT, int64_t 
       const dim3 join((unsigned)ceil_div(pl.chunks, WAVES_PER_WG), (unsigned)std::min<int64_t>(64, ceil_div(ceil_div(D, V), 64)));
       embed_join_kernel<X, Y, V><<<join, dim3(WG_THREADS), 0, s>>>(a);
     }
-    return took(T <= SORT_SMALL ? "embed_grad:small_sort" : "embed_grad:sort", launched());
+    return took(T <= SORT_SMALL ? "embed_grad:ranks" : "embed_grad:sort", launched());
   };
   const auto run = [&](auto x, auto y) {
     constexpr int V = std::min(Elem<decltype(x)>::PER16, Elem<decltype(y)>::PER16);

@@ -87,8 +87,13 @@ def test_embed_grad_of_one_number_and_of_none(T):
 
 def test_embed_grad_of_many_tokens_and_of_a_long_table():
     rng = np.random.default_rng(5)
+    _grad(torch.float32, torch.float32, 900, 4, 8192, False, rng.integers(0, 900, 8192), pad=7)  # the most that are ranked by counting
+    assert tc.last_path() == "embed_grad:ranks"
+    _grad(torch.float32, torch.float32, 900, 4, 8193, False, rng.integers(0, 900, 8193), pad=7)
+    assert tc.last_path() == "embed_grad:sort"
     _grad(torch.float32, torch.float32, 1000, 4, 140001, False, rng.integers(0, 1000, 140001), pad=-1)  # counts summed by a launch of their own
-    _grad(torch.bfloat16, torch.bfloat16, (1 << 21) + 3, 2, 5000, False, rng.integers(0, (1 << 21) + 3, 5000), pad=-1)  # three digits
+    _grad(torch.bfloat16, torch.bfloat16, (1 << 21) + 3, 2, 5000, False, rng.integers(0, (1 << 21) + 3, 5000), pad=-1)
+    _grad(torch.bfloat16, torch.bfloat16, (1 << 21) + 3, 2, 9000, False, rng.integers(0, (1 << 21) + 3, 9000), pad=-1)  # three digits
 
 
 def test_embed_grad_without_tokens():
