@@ -470,7 +470,7 @@ tc_status tc_embed_grad(const void *dO, const int32_t *Idx, void *dLUT,
  * no other is left empty: Id = -1, Wt = 0, Place = -1; places from Off(E) on have Row = -1.  NaN ranks above
  * every number; a token with a NaN or a +inf among its logits has weights of NaN
  * (norm = 1: if one is among the chosen, which it is).
- * 1 <= k <= E; E <= 1023 and k <= 64 (TC_ERR_UNSUPPORTED beyond).
+ * 1 <= k <= E; E <= 1023, k <= 64 and T < 2^28 (TC_ERR_UNSUPPORTED beyond).
  *   workspace  device scratch of at least tc_route_workspace_bytes(...) bytes,
  *              16-byte aligned; NULL where that is 0 (a few tokens).
  */

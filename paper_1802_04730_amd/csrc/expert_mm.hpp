@@ -88,6 +88,7 @@ __device__ __forceinline__ bool expert_tile(const int* off, int E, int R, int bm
       const int mt = (t->hi - t->lo + bm - 1) / bm;
       const int block = (int)(local / (unsigned)(8 * nt)), in = (int)(local % (unsigned)(8 * nt));
       const int rows = min(8, mt - 8 * block);
+      if (rows <= 0 || in / rows >= nt) return false;  // (offsets that go up and down can make more tiles than 32 bits count)
       t->m = 8 * block + in % rows;
       t->n = in / rows;
       return true;

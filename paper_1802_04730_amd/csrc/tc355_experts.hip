@@ -23,6 +23,7 @@ namespace {
 
 constexpr int64_t kMostRows = (int64_t)1 << 30;   // rows, widths: 32-bit indices with room for a tile
 constexpr int64_t kMostWidth = (int64_t)1 << 22;  // of the products: a tile's 256 rows of fp32 within 32-bit offsets
+constexpr int64_t kMostTokens = (int64_t)ROUTE_TOKENS << 23;  // of the router: fewer than 2^32 threads
 constexpr int64_t kMostIndex = ((int64_t)1 << 31) - 1;
 
 inline bool misaligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) != 0; }
@@ -309,7 +310,7 @@ tc_status tc_embed_grad(const void* dO, const int32_t* Idx, void* dLUT, int64_t 
 }
 
 size_t tc_route_workspace_bytes(int64_t T, int64_t E, int64_t k) {
-  if (T <= 0 || E <= 0 || k <= 0 || k > E || E > ROUTE_MOST_E || k > ROUTE_MOST_K || prod_reaches({T, k}, kMostRows)) return 0;
+  if (T <= 0 || E <= 0 || k <= 0 || k > E || E > ROUTE_MOST_E || k > ROUTE_MOST_K || T >= kMostTokens || prod_reaches({T, k}, kMostRows)) return 0;
   return (size_t)route_ws(T, E);
 }
 
@@ -325,7 +326,7 @@ tc_status tc_route(const void* L, float* Wt, int32_t* Id, int32_t* Off, int32_t*
     if (i < 5 && misaligned(out[i])) return TC_ERR_ALIGN;
   }
   if (misaligned(L)) return TC_ERR_ALIGN;
-  if (E > ROUTE_MOST_E || k > ROUTE_MOST_K || prod_reaches({std::max<int64_t>(T, 1), k}, kMostRows) || T > kMostRows) return TC_ERR_UNSUPPORTED;
+  if (E > ROUTE_MOST_E || k > ROUTE_MOST_K || prod_reaches({std::max<int64_t>(T, 1), k}, kMostRows) || T >= kMostTokens) return TC_ERR_UNSUPPORTED;
   const int64_t need = route_ws(T, E);
   if (need && (!workspace || misaligned(workspace) || workspace_bytes < (size_t)need)) return TC_ERR_WORKSPACE;
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
