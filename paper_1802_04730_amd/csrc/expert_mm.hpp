@@ -18,6 +18,12 @@
 // both operands keep it.  The operands are exchanged (weights first), so that a lane's four results are neighbours in a row of the output.
 //
 // Sums are fp32 in the matrix core's accumulators whatever the storage, and each output is rounded once.
+//
+// Measured, bfloat16: one matrix of 8192^3 863 us forward (1274 TFLOP/s, tile of 256), 1045 dX, 1092 dW (128); 32 experts of 512 rows each, N = 2048,
+// K = 4096: 285, 382, 474 us; of uneven shares 376-430, 390-430, 453-486: the last round of tiles, and last rows of experts, are
+// not full.  fp32, 2100 rows of 12 experts, 1001 x 517: 40, 52, 44 us.  Tried and left: two stages with all fragments read at once (352
+// us forward at uneven shares where this takes 376), four stages of 64 bytes (404), 16 wavefronts a tile of 256 (spills), tiles of 256 x 128
+// in a ring of three (1088 TFLOP/s at 8192^3, more lost at ragged ends), the last round's tiles shared by two workgroups (no gain).
 #pragma once
 #include "expert_types.hpp"
 

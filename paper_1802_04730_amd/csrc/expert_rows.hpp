@@ -4,6 +4,8 @@
 // A workgroup computes 16 RT rows by 16 CT columns of one expert; its wavefronts share the reduction, in steps of 64 bytes of a row.
 // Operands go from memory to registers in the matrix instruction's layout -- nothing is used twice, so LDS would only be a
 // detour -- with EROWS_AHEAD steps requested together, and the partial tiles meet once, in LDS, in the wavefronts' order.
+// RT = 1 up to 16 rows an expert on average, 4 below 64: from there on the tiles of expert_mm.hpp read less.  Measured: 32 rows of
+// 8 experts, N = 4096, K = 2048 in bfloat16 22.6-23.9 us = 5.6-5.9 TB/s of weights (tiles of 128: 39.8 us); 256 rows 40, 500 rows 61.
 #pragma once
 #include "expert_mm.hpp"
 
