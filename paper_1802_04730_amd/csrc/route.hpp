@@ -8,7 +8,7 @@
 // NaN ranks above every number, as does nothing else; a row with a NaN or a +inf has weights of NaN, as the formula has.
 // The selection compares the logits themselves, as integers that order as they do (-0 as +0), so that rounding never decides.
 //
-// A group of 16 lanes (64 for more than 128 experts) takes a token, each lane the logits lane, lane + G, ..: k rounds find the
+// A group of 16 lanes (64 for more than 128 experts) takes a token, each lane a few neighbouring logits: k rounds find the
 // largest of what is left by exchange inside the group (moves between lanes of a row of 16, without LDS).  What bounds it is those
 // rounds' latency, not the logits' bytes.  A workgroup takes ROUTE_TOKENS tokens and counts its slots per expert; the counts are
 // summed over the workgroups, and a last launch places the slots (key_sort.hpp's ranks by ballot).  Up to ROUTE_ALONE tokens
@@ -66,6 +66,23 @@ __device__ __forceinline__ float sum_of(float a, float b) { return a + b; }
 __device__ __forceinline__ unsigned larger(unsigned a, unsigned b) { return a > b ? a : b; }
 __device__ __forceinline__ int smaller(int a, int b) { return a < b ? a : b; }
 
+// A lane's logits: V neighbours from column c on, in as few loads as they fit; -inf past the end.
+template <typename T, int V>
+__device__ __forceinline__ void load_logits(const T* row, int c, int E, float (&x)[V]) {
+  constexpr int P = V < Elem<T>::PER16 ? V : Elem<T>::PER16;
+  if (c + V <= E) {
+#pragma unroll
+    for (int h = 0; h < V; h += P) {
+      const Pack<T, P> v = load_pack<T, P>(row + c + h);
+#pragma unroll
+      for (int i = 0; i < P; i++) x[h + i] = (float)v.e[i];
+    }
+  } else {
+#pragma unroll
+    for (int v = 0; v < V; v++) x[v] = c + v < E ? (float)row[c + v] : -__builtin_inff();
+  }
+}
+
 // The places of a workgroup's slots: Id of the tokens of workgroup `tile`, all threads.
 __device__ __forceinline__ void route_place(const RouteArgs& p, int tile, const int* start, int* count) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, bins = 1 << p.bits;
@@ -118,10 +135,9 @@ __global__ __launch_bounds__(WG_THREADS) void route_kernel(RouteArgs p) {
     float x[V];
     unsigned key[V];
     float most = -__builtin_inff();
+    load_logits<T, V>(L + t * p.E, lane * V, p.E, x);
 #pragma unroll
     for (int v = 0; v < V; v++) {
-      const int e = v * G + lane;
-      x[v] = e < p.E ? (float)L[t * p.E + e] : -__builtin_inff();
       key[v] = route_order(x[v]);
       most = fmaxf(most, x[v]);
     }
@@ -144,12 +160,12 @@ __global__ __launch_bounds__(WG_THREADS) void route_kernel(RouteArgs p) {
       int at = 0x7fffffff;
 #pragma unroll
       for (int v = V - 1; v >= 0; v--)
-        if (key[v] == best) at = v * G + lane;
+        if (key[v] == best) at = lane * V + v;
       at = group_all<G>(at, smaller);
       float mine = 0.0f;
 #pragma unroll
       for (int v = 0; v < V; v++)
-        if (best && at == v * G + lane) {
+        if (best && at == lane * V + v) {
           key[v] = 0;
           mine = x[v];
         }
@@ -217,25 +233,30 @@ __global__ __launch_bounds__(WG_THREADS) void route_grad_kernel(RouteGradArgs p)
   float x[V], g[V];
   bool chosen[V];
   float most = -__builtin_inff();
+  load_logits<T, V>(L, lane * V, p.E, x);
 #pragma unroll
   for (int v = 0; v < V; v++) {
-    const int e = v * G + lane;
-    x[v] = e < p.E ? (float)L[e] : -__builtin_inff();
     most = fmaxf(most, x[v]);
     g[v] = 0.0f;
     chosen[v] = false;
   }
   most = group_all<G>(most, most_of);
   if (most == -__builtin_inff()) most = 0.0f;
-  for (int i = 0; i < p.k; i++) {
-    const int id = p.Id[t * p.k + i];
-    const float d = p.dWt[t * p.k + i];
+  for (int i0 = 0; i0 < p.k; i0 += G) {  // a slot a lane, handed round
+    const int i = min(i0 + lane, p.k - 1);
+    const int ids = p.Id[t * p.k + i];
+    const float ds = p.dWt[t * p.k + i];
+    const int n = min(G, p.k - i0);
+    for (int j = 0; j < n; j++) {
+      const int id = __shfl(ids, j, G);
+      const float d = __shfl(ds, j, G);
 #pragma unroll
-    for (int v = 0; v < V; v++)
-      if (id == v * G + lane) {
-        g[v] = d;
-        chosen[v] = true;
-      }
+      for (int v = 0; v < V; v++)
+        if (id == lane * V + v) {
+          g[v] = d;
+          chosen[v] = true;
+        }
+    }
   }
   float sum = 0.0f, inner = 0.0f;
 #pragma unroll
@@ -247,13 +268,26 @@ __global__ __launch_bounds__(WG_THREADS) void route_grad_kernel(RouteGradArgs p)
   sum = group_all<G>(sum, sum_of);
   inner = group_all<G>(inner, sum_of);
   if (sum == 0.0f) sum = 1.0f;  // (a row of nothing, or without slots)
-  inner /= sum;
+  const float share = 1.0f / sum;
+  inner *= share;
+  T* const out = static_cast<T*>(p.dL) + t * p.E;
+  T o[V];
 #pragma unroll
-  for (int v = 0; v < V; v++) {
-    const int e = v * G + lane;
-    if (e >= p.E) continue;
-    const float share = !p.norm || chosen[v] ? x[v] / sum : 0.0f;
-    static_cast<T*>(p.dL)[t * p.E + e] = narrow<T>(share * ((chosen[v] ? g[v] : 0.0f) - inner));
+  for (int v = 0; v < V; v++) o[v] = narrow<T>((!p.norm || chosen[v] ? x[v] * share : 0.0f) * (g[v] - inner));  // (g: 0 where not chosen)
+  const int c = lane * V;
+  if (c + V <= p.E) {
+    constexpr int P = V < Elem<T>::PER16 ? V : Elem<T>::PER16;
+#pragma unroll
+    for (int h = 0; h < V; h += P) {
+      Pack<T, P> v;
+#pragma unroll
+      for (int i = 0; i < P; i++) v.e[i] = o[h + i];
+      *reinterpret_cast<Pack<T, P>*>(out + c + h) = v;
+    }
+  } else {
+#pragma unroll
+    for (int v = 0; v < V; v++)
+      if (c + v < p.E) out[c + v] = o[v];
   }
 }
 
