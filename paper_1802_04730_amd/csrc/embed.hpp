@@ -10,7 +10,7 @@
 // inside a chunk go to the table; the ends that a chunk shares with its neighbours go to a workspace, and a second launch joins them, chunk by
 // chunk: language has words that make up a large part of a batch.  No atomics, one order for every sum.  Rows of numbers that do not occur are
 // written with zeros by workgroups of their own in the same launch, or left alone where the gradient is added to what is there.
-// (A group of lanes per row of the table, empty or not: 402 us against 243 and 10 at 32768 tokens of 2048 bfloat16, a table of 131072 rows in fp32: three
+// (A group of lanes per row of the table, empty or not: 402 us against 233 and 10 at 32768 tokens of 2048 bfloat16, a table of 131072 rows in fp32: three
 // dependent trips to memory a row.)
 #pragma once
 #include "expert_types.hpp"
@@ -118,18 +118,19 @@ __global__ __launch_bounds__(WG_THREADS) void embed_grad_kernel(EmbedGradArgs p)
     return;
   }
   // a chunk for each group of lanes: its numbers (with the neighbours') and tokens
-  __shared__ int keys[WG_THREADS][EMBED_CHUNK + 2 + 1], tokens[WG_THREADS][EMBED_CHUNK + 1];  // (odd rows: groups in different banks)
+  extern __shared__ int mem[];  // groups of chunk + 3 numbers, then of chunk + 1 tokens (odd rows: groups in different banks)
+  int *const keys = mem + group * (p.chunk + 3), *const tokens = mem + groups * (p.chunk + 3) + group * (p.chunk + 1);
   const int64_t chunk = (int64_t)blockIdx.x * groups + group;
   const int64_t lo = chunk * p.chunk;
   const int n = (int)max((int64_t)0, min((int64_t)p.chunk, p.T - lo));
   for (int j = lane; j < n + 2 && n; j += p.lpr) {
     const int64_t at = lo - 1 + j;
-    keys[group][j] = at >= 0 && at < p.T ? p.key[at] : -1;  // (-1: nobody's)
-    if (j < n) tokens[group][j] = p.order[lo + j];
+    keys[j] = at >= 0 && at < p.T ? p.key[at] : -1;  // (-1: nobody's)
+    if (j < n) tokens[j] = p.order[lo + j];
   }
   __syncthreads();
   if (n == 0) return;
-  const int* const key = keys[group] + 1;
+  const int* const key = keys + 1;
   constexpr int NB = 8;  // rows in flight
   for (int64_t c = lane; c * V < p.D; c += p.lpr) {
     const RowUnit<V> u(c, p.D);
@@ -141,7 +142,7 @@ __global__ __launch_bounds__(WG_THREADS) void embed_grad_kernel(EmbedGradArgs p)
       if (key[r0] >= p.E) break;  // (tokens of no row come last)
       Pack<T, V> v[NB];
 #pragma unroll
-      for (int j = 0; j < NB; j++) v[j] = load_unit<T, V>(static_cast<const T*>(p.dO) + (int64_t)tokens[group][min(r0 + j, n - 1)] * p.D, u);
+      for (int j = 0; j < NB; j++) v[j] = load_unit<T, V>(static_cast<const T*>(p.dO) + (int64_t)tokens[min(r0 + j, n - 1)] * p.D, u);
 #pragma unroll
       for (int j = 0; j < NB; j++) {
         const int r = r0 + j;

@@ -13,8 +13,8 @@
 // rounds' latency, not the logits' bytes.  A workgroup takes ROUTE_TOKENS tokens and counts its slots per expert; the counts are
 // summed over the workgroups, and a last launch places the slots (key_sort.hpp's ranks by ballot).  Up to ROUTE_ALONE tokens
 // all of it is one workgroup's, in one launch.  No atomics on memory; integer ones in LDS.  Measured: 16 tokens of 64 experts, 4
-// chosen, 5.0 us; 16384 of 128, 8 chosen, 13.6 for the selection (29 by exchange through LDS), 3.9 for the sums, 6.6 for the places (63 where every
-// workgroup added the earlier ones' counts up), 10.6 for the gradient.
+// chosen, 4.7 us; 16384 of 128, 8 chosen, 12.8 for the selection (29 by exchange through LDS), 4.2 for the sums, 6.3 for the places (63 where every
+// workgroup added the earlier ones' counts up), 9.6 for the gradient.
 #pragma once
 #include "expert_types.hpp"
 #include "key_sort.hpp"

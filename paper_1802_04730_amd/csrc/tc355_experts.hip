@@ -295,7 +295,8 @@ tc_status tc_embed_grad(const void* dO, const int32_t* Idx, void* dLUT, int64_t 
       const tc_status st = sort_tokens(pl, Idx, T, E, pad, ws, &a.key, &a.order, s);
       if (st != TC_OK) return st;
     }
-    embed_grad_kernel<X, Y, V><<<dim3((unsigned)grid), dim3(WG_THREADS), 0, s>>>(a);
+    const size_t lds = (size_t)(WG_THREADS / a.lpr) * (2 * a.chunk + 4) * 4;
+    embed_grad_kernel<X, Y, V><<<dim3((unsigned)grid), dim3(WG_THREADS), lds, s>>>(a);
     if (pl.chunks > 1) {
       const dim3 join((unsigned)ceil_div(pl.chunks, WAVES_PER_WG), (unsigned)std::min<int64_t>(64, ceil_div(ceil_div(D, V), 64)));
       embed_join_kernel<X, Y, V><<<join, dim3(WG_THREADS), 0, s>>>(a);

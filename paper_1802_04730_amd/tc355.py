@@ -400,6 +400,11 @@ def _typed(t, name: str, dims: int, dtype=None):
     return t.data_ptr()
 
 
+def _grad_of(t, name: str, dims: int, dtype):
+    """The same for a gradient, which may be kept in float32 whatever the type of what it is taken from."""
+    return _typed(t, name, dims, None if getattr(t, "dtype", None) is torch.float32 else dtype)
+
+
 def _fit(ok: bool, where: str) -> None:
     if not ok:
         raise ValueError("%s: shapes do not fit" % where)
@@ -437,7 +442,7 @@ def tc_embed_grad(dO, Idx, dLUT, workspace, scale: float = 1.0, pad: int = -1, a
         status = _FAST.embed_grad(_AT["tc_embed_grad"], dO, Idx, dLUT, workspace, scale, pad, add, stream)
         if status >= 0:
             return _check(status, "tc_embed_grad")
-    d, i, g = _typed(dO, "dO", 2), _typed(Idx, "Idx", 1, torch.int32), _typed(dLUT, "dLUT", 2, None if dLUT.dtype is torch.float32 else dO.dtype)
+    d, i, g = _typed(dO, "dO", 2), _typed(Idx, "Idx", 1, torch.int32), _grad_of(dLUT, "dLUT", 2, dO.dtype)
     (T, D), E = dO.shape, dLUT.shape[0]
     _fit(dLUT.shape[1] == D and Idx.shape[0] == T, "tc_embed_grad")
     wp, wn = _workspace(workspace)
@@ -519,7 +524,7 @@ def tc_expert_mm_grad_w(dY, X, Off, Row, dW, workspace=None, add: bool = False, 
             return _check(status, "tc_expert_mm_grad_w")
     i32 = torch.int32
     args = (_typed(dY, "dY", 2), _typed(X, "X", 2, dY.dtype), _typed(Off, "Off", 1, i32), None if Row is None else _typed(Row, "Row", 1, i32),
-            _typed(dW, "dW", 3, None if dW.dtype is torch.float32 else dY.dtype))
+            _grad_of(dW, "dW", 3, dY.dtype))
     (R, N), (T, K), E = dY.shape, X.shape, dW.shape[0]
     _fit(tuple(dW.shape) == (E, N, K) and Off.shape[0] == E + 1 and (T if Row is None else Row.shape[0]) == R, "tc_expert_mm_grad_w")
     wp, wn = _workspace(workspace)
