@@ -128,3 +128,34 @@ def test_too_small_a_workspace_only_costs_time():
     tc.tc_expert_mm_grad_w(dY, X, _ints([0, R]), None, dW, _bytes(4 * E * N * K))  # (one part's)
     assert tc.last_path() == "expert_mm_grad_w:tile"
     _close(dW, *_weights(dY.double(), X.double(), [0, R], None), R, torch.bfloat16)
+
+
+def test_rows_beyond_4_gb():
+    """Rows taken from both ends of a matrix of more than 4 GB: no tile addresses them by 32 bits."""
+    T, R, E, N, K = (1 << 20) + 9, 4100, 3, 3600, 2056
+    off = _offsets(R, E, 9)
+    places = torch.tensor([0, 1, 1 << 19, (1 << 20) - 1, 1 << 20, T - 1], device="cuda")
+    X = torch.empty((T, K), dtype=torch.bfloat16, device="cuda")
+    X[places] = _rand((len(places), K), torch.bfloat16, 1)
+    Row = places[torch.from_numpy(np.random.default_rng(2).integers(0, len(places), R)).cuda()].to(torch.int32)
+    W, Y, dY = _rand((E, N, K), torch.bfloat16, 3, K ** -0.5), torch.empty((R, N), dtype=torch.bfloat16, device="cuda"), _rand((R, N), torch.bfloat16, 4)
+    tc.tc_expert_mm(X, W, _ints(off), Row, Y)
+    x, w = X[Row.long()].double(), W.double()
+    _close(Y, *_by_expert(off, R, N, lambda e, a, b: (x[a:b] @ w[e].t(), x[a:b].abs() @ w[e].abs().t())), K, torch.bfloat16)
+    tc.tc_expert_mm_grad_w(dY, X, _ints(off), Row, W)
+    _close(W, *_weights(dY.double(), x, off, None), R, torch.bfloat16)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_results_beyond_the_type_and_far_below_one(dtype):
+    """Sums that no value of the type holds become infinite, as by one rounding; products of small values are not lost on the way."""
+    R, E, N, K = 200, 2, 136, 64
+    big, small = (3e38, 1e-18) if dtype is torch.bfloat16 else (6e4, 1e-3)
+    off = _ints([0, 90, R])
+    for value, other in ((big, 1.0), (small, small)):
+        X, W = torch.full((R, K), value, dtype=dtype, device="cuda"), torch.full((E, N, K), other, dtype=dtype, device="cuda")
+        Y = torch.empty((R, N), dtype=dtype, device="cuda")
+        tc.tc_expert_mm(X, W, off, None, Y)
+        want = (X.double() @ W[0].double().t()).float().to(dtype)
+        assert torch.equal(Y, want) or bool(((Y.double() - want.double()).abs() <= 2 * UNIT[dtype] * want.double().abs()).all())
+        assert bool(torch.isinf(Y).all()) == (value == big)
