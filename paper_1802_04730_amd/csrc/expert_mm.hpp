@@ -465,6 +465,32 @@ __device__ __forceinline__ void emm_store(TO* p, int left, bool whole, f4 v) {
   }
 }
 
+// A tile of 16-bit results by whole lines: through LDS (chunk c of row r in slot c ^ (r & 7)), then 16 bytes a lane, neighbours along
+// the row.  put(row, column, values): stores 8 neighbours of the tile.
+template <typename T, int BM, int BN, int THREADS, int MI, int NI, typename Put>
+__device__ __forceinline__ void emm_store_lines(lds_char* lds, const f4 (&acc)[MI][NI], int rm, int cn, Put put) {
+  const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, q = lane >> 4;
+  typedef typename Elem<T>::v4 v4;
+  __syncthreads();  // (everyone has read the last stage)
+#pragma unroll
+  for (int m = 0; m < MI; m++)
+#pragma unroll
+    for (int n = 0; n < NI; n++) {
+      v4 o;
+#pragma unroll
+      for (int x = 0; x < 4; x++) o[x] = narrow<T>(acc[m][n][x]);
+      const int r = rm + 16 * m + i, c = cn + 16 * n + 4 * q;
+      *(__attribute__((address_space(3))) v4*)(lds + r * (BN * 2) + (((c >> 3) ^ (r & 7)) * 16) + (q & 1) * 8) = o;
+    }
+  __syncthreads();
+#pragma unroll 4
+  for (int x = tid; x < BM * BN / 8; x += THREADS) {
+    const int r = x / (BN / 8), c = x % (BN / 8);
+    const u4 v = *(const __attribute__((address_space(3))) u4*)(lds + r * (BN * 2) + ((c ^ (r & 7)) * 16));
+    put(r, 8 * c, __builtin_bit_cast(typename Elem<T>::v8, v));
+  }
+}
+
 // ---- kernels ---------------------------------------------------------------------------------------------------------------
 
 struct ExpertRowsArgs {
@@ -515,6 +541,32 @@ __global__ __launch_bounds__(64 * WM * WN) void expert_rows_tile_kernel(ExpertRo
   }
   const int stages = owned ? (p.Q + OpA::BK - 1) / OpA::BK : 0;
   emm_loop<T, MODE, D, MI, NI>(a, b, (lds_char*)lds, stages, rm, cn, wave, lane, acc);
+  if constexpr (sizeof(T) == 2 && MODE == EMM_WHOLE) {
+    if ((p.NO & 7) == 0) {
+      if (p.relu) {
+#pragma unroll
+        for (int m = 0; m < MI; m++)
+#pragma unroll
+          for (int n = 0; n < NI; n++)
+#pragma unroll
+            for (int x = 0; x < 4; x++) acc[m][n][x] = acc[m][n][x] > 0.0f ? acc[m][n][x] : 0.0f;  // (NaN and -0 give +0)
+      }
+      emm_store_lines<T, BM, BN, 64 * NW>((lds_char*)lds, acc, rm, cn, [&](int row, int col, typename Elem<T>::v8 v) {
+        typedef typename Elem<T>::v8 v8;
+        const int r = m0 + row, c = n0 + col;
+        if (r >= hi || c >= p.NO) return;
+        const int64_t o = (int64_t)r * p.NO + c;
+        if (p.row && owned && (p.row[r] < 0 || p.row[r] >= p.T)) v = v8{};  // (a row of zeros)
+        if (p.gate && owned) {
+          const v8 h = *reinterpret_cast<const v8*>(static_cast<const T*>(p.gate) + o);
+#pragma unroll
+          for (int x = 0; x < 8; x++) v[x] = static_cast<float>(h[x]) > 0.0f ? v[x] : static_cast<T>(0.0f);
+        }
+        __builtin_nontemporal_store(v, reinterpret_cast<v8*>(static_cast<T*>(p.C) + o));
+      });
+      return;
+    }
+  }
   const int i = lane & 15, q = lane >> 4;
   const bool by4 = (p.NO & 3) == 0;
 #pragma unroll
@@ -592,6 +644,16 @@ __global__ __launch_bounds__(64 * WM * WN) void expert_weights_kernel(ExpertWeig
   if constexpr (LIST) b.template begin<MODE>(static_cast<const T*>(p.X), p.K, p.row + lo, rows, p.T, n0, p.K, wave, lane);
   else b.template begin<MODE>(static_cast<const T*>(p.X) + (int64_t)lo * p.K, p.K, nullptr, rows, rows, n0, p.K, wave, lane);
   emm_loop<T, MODE, D, MI, NI>(a, b, (lds_char*)lds, (rows + OpA::BK - 1) / OpA::BK, rm, cn, wave, lane, acc);
+  if constexpr (sizeof(T) == 2 && __is_same(T, TO) && MODE == EMM_WHOLE) {
+    if (!p.add) {
+      T* const whole = static_cast<T*>(p.dW) + (int64_t)e * p.N * p.K;  // (no parts: those are fp32)
+      emm_store_lines<T, BM, BN, 64 * NW>((lds_char*)lds, acc, rm, cn, [&](int row, int col, typename Elem<T>::v8 v) {
+        const int r = m0 + row, c = n0 + col;
+        if (r < p.N && c < p.K) __builtin_nontemporal_store(v, reinterpret_cast<typename Elem<T>::v8*>(whole + (int64_t)r * p.K + c));
+      });
+      return;
+    }
+  }
   const int i = lane & 15, q = lane >> 4;
   const bool by4 = (p.K & 3) == 0;
   TO* out = static_cast<TO*>(p.dW) + ((int64_t)blockIdx.y * p.E + e) * p.N * p.K;
