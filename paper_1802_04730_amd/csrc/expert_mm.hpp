@@ -450,7 +450,7 @@ __device__ __forceinline__ void emm_loop(A& a, B& b, lds_char* lds, int stages, 
 }
 
 // Four neighbours of an output row from column n on, of which `left` are there.  (Through the caches: these are parts of lines, which
-// cost a write to memory each where they pass them by: forward and gradients of (E,R,N,K) = (32,16384,2048,4096) 1170 us, so 1320.)
+// cost a write to memory each where they pass them by: forward and gradients of (E,R,N,K) = (32,16384,2048,4096) 1320 us instead of 1170.)
 template <typename TO>
 __device__ __forceinline__ void emm_store(TO* p, int left, bool whole, f4 v) {
   if (whole) {
@@ -465,12 +465,14 @@ __device__ __forceinline__ void emm_store(TO* p, int left, bool whole, f4 v) {
   }
 }
 
-// A tile of 16-bit results by whole lines: through LDS (chunk c of row r in slot c ^ (r & 7)), then 16 bytes a lane, neighbours along
-// the row.  put(row, column, values): stores 8 neighbours of the tile.
-template <typename T, int BM, int BN, int THREADS, int MI, int NI, typename Put>
+// A tile of results by whole lines: through LDS (16-byte chunk c of row r in slot c ^ (r & 7)), then 16 bytes a lane, neighbours along the
+// row, past the caches.  put(row, column, values): stores 16 bytes of the tile.  (The accumulators' own pieces of 8 or 16 bytes: the
+// gradient of the weights of (E,R,N,K) = (32,16384,2048,4096) in bfloat16 486 us instead of 401, 8192^3 forward 863 instead of 785.)
+template <typename TO, int BM, int BN, int THREADS, int MI, int NI, typename Put>
 __device__ __forceinline__ void emm_store_lines(lds_char* lds, const f4 (&acc)[MI][NI], int rm, int cn, Put put) {
+  constexpr int PER = Elem<TO>::PER16, ROW = BN * sizeof(TO);
   const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, q = lane >> 4;
-  typedef typename Elem<T>::v4 v4;
+  typedef typename Elem<TO>::v4 v4;
   __syncthreads();  // (everyone has read the last stage)
 #pragma unroll
   for (int m = 0; m < MI; m++)
@@ -478,16 +480,16 @@ __device__ __forceinline__ void emm_store_lines(lds_char* lds, const f4 (&acc)[M
     for (int n = 0; n < NI; n++) {
       v4 o;
 #pragma unroll
-      for (int x = 0; x < 4; x++) o[x] = narrow<T>(acc[m][n][x]);
+      for (int x = 0; x < 4; x++) o[x] = narrow<TO>(acc[m][n][x]);
       const int r = rm + 16 * m + i, c = cn + 16 * n + 4 * q;
-      *(__attribute__((address_space(3))) v4*)(lds + r * (BN * 2) + (((c >> 3) ^ (r & 7)) * 16) + (q & 1) * 8) = o;
+      *(__attribute__((address_space(3))) v4*)(lds + r * ROW + (((c / PER) ^ (r & 7)) * 16) + c % PER * (int)sizeof(TO)) = o;
     }
   __syncthreads();
 #pragma unroll 4
-  for (int x = tid; x < BM * BN / 8; x += THREADS) {
-    const int r = x / (BN / 8), c = x % (BN / 8);
-    const u4 v = *(const __attribute__((address_space(3))) u4*)(lds + r * (BN * 2) + ((c ^ (r & 7)) * 16));
-    put(r, 8 * c, __builtin_bit_cast(typename Elem<T>::v8, v));
+  for (int x = tid; x < BM * BN / PER; x += THREADS) {
+    const int r = x / (BN / PER), c = x % (BN / PER);
+    const u4 v = *(const __attribute__((address_space(3))) u4*)(lds + r * ROW + ((c ^ (r & 7)) * 16));
+    put(r, PER * c, __builtin_bit_cast(typename Elem<TO>::v16, v));
   }
 }
 
@@ -541,8 +543,10 @@ __global__ __launch_bounds__(64 * WM * WN) void expert_rows_tile_kernel(ExpertRo
   }
   const int stages = owned ? (p.Q + OpA::BK - 1) / OpA::BK : 0;
   emm_loop<T, MODE, D, MI, NI>(a, b, (lds_char*)lds, stages, rm, cn, wave, lane, acc);
-  if constexpr (sizeof(T) == 2 && MODE == EMM_WHOLE) {
-    if ((p.NO & 7) == 0) {
+  if constexpr (MODE != EMM_NARROW) {
+    typedef typename Elem<T>::v16 v16;
+    constexpr int PER = Elem<T>::PER16;
+    if (p.NO % PER == 0) {
       if (p.relu) {
 #pragma unroll
         for (int m = 0; m < MI; m++)
@@ -551,18 +555,17 @@ __global__ __launch_bounds__(64 * WM * WN) void expert_rows_tile_kernel(ExpertRo
 #pragma unroll
             for (int x = 0; x < 4; x++) acc[m][n][x] = acc[m][n][x] > 0.0f ? acc[m][n][x] : 0.0f;  // (NaN and -0 give +0)
       }
-      emm_store_lines<T, BM, BN, 64 * NW>((lds_char*)lds, acc, rm, cn, [&](int row, int col, typename Elem<T>::v8 v) {
-        typedef typename Elem<T>::v8 v8;
+      emm_store_lines<T, BM, BN, 64 * NW>((lds_char*)lds, acc, rm, cn, [&](int row, int col, v16 v) {
         const int r = m0 + row, c = n0 + col;
         if (r >= hi || c >= p.NO) return;
         const int64_t o = (int64_t)r * p.NO + c;
-        if (p.row && owned && (p.row[r] < 0 || p.row[r] >= p.T)) v = v8{};  // (a row of zeros)
+        if (p.row && owned && (p.row[r] < 0 || p.row[r] >= p.T)) v = v16{};  // (a row of zeros)
         if (p.gate && owned) {
-          const v8 h = *reinterpret_cast<const v8*>(static_cast<const T*>(p.gate) + o);
+          const v16 h = *reinterpret_cast<const v16*>(static_cast<const T*>(p.gate) + o);
 #pragma unroll
-          for (int x = 0; x < 8; x++) v[x] = static_cast<float>(h[x]) > 0.0f ? v[x] : static_cast<T>(0.0f);
+          for (int x = 0; x < PER; x++) v[x] = static_cast<float>(h[x]) > 0.0f ? v[x] : static_cast<T>(0.0f);
         }
-        __builtin_nontemporal_store(v, reinterpret_cast<v8*>(static_cast<T*>(p.C) + o));
+        __builtin_nontemporal_store(v, reinterpret_cast<v16*>(static_cast<T*>(p.C) + o));
       });
       return;
     }
@@ -644,19 +647,32 @@ __global__ __launch_bounds__(64 * WM * WN) void expert_weights_kernel(ExpertWeig
   if constexpr (LIST) b.template begin<MODE>(static_cast<const T*>(p.X), p.K, p.row + lo, rows, p.T, n0, p.K, wave, lane);
   else b.template begin<MODE>(static_cast<const T*>(p.X) + (int64_t)lo * p.K, p.K, nullptr, rows, rows, n0, p.K, wave, lane);
   emm_loop<T, MODE, D, MI, NI>(a, b, (lds_char*)lds, (rows + OpA::BK - 1) / OpA::BK, rm, cn, wave, lane, acc);
-  if constexpr (sizeof(T) == 2 && __is_same(T, TO) && MODE == EMM_WHOLE) {
-    if (!p.add) {
-      T* const whole = static_cast<T*>(p.dW) + (int64_t)e * p.N * p.K;  // (no parts: those are fp32)
-      emm_store_lines<T, BM, BN, 64 * NW>((lds_char*)lds, acc, rm, cn, [&](int row, int col, typename Elem<T>::v8 v) {
+  TO* const out = static_cast<TO*>(p.dW) + ((int64_t)blockIdx.y * p.E + e) * p.N * p.K;
+  if constexpr (MODE != EMM_NARROW) {
+    typedef typename Elem<TO>::v16 v16;
+    // (16-bit results that are added to are rounded once, from the accumulators, below)
+    if (p.K % Elem<TO>::PER16 == 0 && !(p.add && sizeof(TO) == 2)) {
+      const auto at = [&](int row, int col) -> v16* {
         const int r = m0 + row, c = n0 + col;
-        if (r < p.N && c < p.K) __builtin_nontemporal_store(v, reinterpret_cast<typename Elem<T>::v8*>(whole + (int64_t)r * p.K + c));
-      });
+        return r < p.N && c < p.K ? reinterpret_cast<v16*>(out + (int64_t)r * p.K + c) : nullptr;
+      };
+      if (sizeof(TO) == 4 && p.parts > 1) {  // (read back at once)
+        emm_store_lines<TO, BM, BN, 64 * NW>((lds_char*)lds, acc, rm, cn, [&](int row, int col, v16 v) {
+          if (v16* o = at(row, col)) *o = v;
+        });
+      } else {
+        emm_store_lines<TO, BM, BN, 64 * NW>((lds_char*)lds, acc, rm, cn, [&](int row, int col, v16 v) {
+          if (v16* o = at(row, col)) {
+            if (p.add) v += *o;
+            __builtin_nontemporal_store(v, o);
+          }
+        });
+      }
       return;
     }
   }
   const int i = lane & 15, q = lane >> 4;
   const bool by4 = (p.K & 3) == 0;
-  TO* out = static_cast<TO*>(p.dW) + ((int64_t)blockIdx.y * p.E + e) * p.N * p.K;
 #pragma unroll
   for (int m = 0; m < MI; m++) {
     const int r = m0 + rm + 16 * m + i;
@@ -684,10 +700,15 @@ __global__ __launch_bounds__(WG_THREADS) void expert_weights_join_kernel(const f
   if (at >= n) return;
   const int left = (int)min((int64_t)4, n - at);
   f4 v = {0, 0, 0, 0};
-  for (int s = 0; s < parts; s++)
+  if (left == 4) {
+#pragma unroll 4
+    for (int s = 0; s < parts; s++) v += __builtin_bit_cast(f4, load_pack<float, 4>(part + s * n + at));
+  } else {
+    for (int s = 0; s < parts; s++)
 #pragma unroll
-    for (int x = 0; x < 4; x++)
-      if (x < left) v[x] += part[s * n + at + x];
+      for (int x = 0; x < 4; x++)
+        if (x < left) v[x] += part[s * n + at + x];
+  }
   TO* o = static_cast<TO*>(dW) + at;
   if (add) {
 #pragma unroll

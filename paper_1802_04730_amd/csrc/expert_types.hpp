@@ -14,17 +14,20 @@ typedef unsigned u4 __attribute__((ext_vector_type(4)));
 
 template <typename T> struct Elem;
 template <> struct Elem<float> {
-  typedef float v4 __attribute__((ext_vector_type(4)));  // 16 bytes
+  typedef float v4 __attribute__((ext_vector_type(4)));
+  typedef v4 v16;  // 16 bytes
   static constexpr int PER16 = 4;
 };
 template <> struct Elem<bf16> {
   typedef bf16 v4 __attribute__((ext_vector_type(4)));
   typedef bf16 v8 __attribute__((ext_vector_type(8)));
+  typedef v8 v16;
   static constexpr int PER16 = 8;
 };
 template <> struct Elem<f16> {
   typedef f16 v4 __attribute__((ext_vector_type(4)));
   typedef f16 v8 __attribute__((ext_vector_type(8)));
+  typedef v8 v16;
   static constexpr int PER16 = 8;
 };
 
