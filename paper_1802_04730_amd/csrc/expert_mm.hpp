@@ -19,11 +19,12 @@
 //
 // Sums are fp32 in the matrix core's accumulators whatever the storage, and each output is rounded once.
 //
-// Measured, bfloat16: one matrix of 8192^3 863 us forward (1274 TFLOP/s, tile of 256), 1045 dX, 1092 dW (128); 32 experts of 512 rows each, N = 2048,
-// K = 4096: 285, 382, 474 us; of uneven shares 376-430, 390-430, 453-486: the last round of tiles, and last rows of experts, are
-// not full.  fp32, 2100 rows of 12 experts, 1001 x 517: 40, 52, 44 us.  Tried and left: two stages with all fragments read at once (352
-// us forward at uneven shares where this takes 376), four stages of 64 bytes (404), 16 wavefronts a tile of 256 (spills), tiles of 256 x 128
-// in a ring of three (1088 TFLOP/s at 8192^3, more lost at ragged ends), the last round's tiles shared by two workgroups (no gain).
+// Measured, bfloat16: one matrix of 8192^3 785 us forward (1400 TFLOP/s, tile of 256), 1024 dX, 1081 dW (128); 32 experts of 512 rows each, N = 2048,
+// K = 4096: 282, 375, 382 us; of uneven shares 369-410, 360-413, 389-404: the last round of tiles, and last rows of experts, are
+// not full.  fp32, 2100 rows of 12 experts, 1001 x 517: 40, 50, 44 us.  Tried and left: two stages with all fragments read at once, four
+// stages of 64 bytes (404 us forward at uneven shares where two of 128 took 352), 16 wavefronts a tile of 256 (spills), tiles of 256 x 128
+// in a ring of three (1088 TFLOP/s at 8192^3 where this then reached 1268, more lost at ragged ends), the last round's tiles shared by two
+// workgroups, and the next tile's first stages requested before this one is stored (no gain).
 #pragma once
 #include "expert_types.hpp"
 
@@ -467,7 +468,7 @@ __device__ __forceinline__ void emm_store(TO* p, int left, bool whole, f4 v) {
 
 // A tile of results by whole lines: through LDS (16-byte chunk c of row r in slot c ^ (r & 7)), then 16 bytes a lane, neighbours along the
 // row, past the caches.  put(row, column, values): stores 16 bytes of the tile.  (The accumulators' own pieces of 8 or 16 bytes: the
-// gradient of the weights of (E,R,N,K) = (32,16384,2048,4096) in bfloat16 486 us instead of 401, 8192^3 forward 863 instead of 785.)
+// gradient of the weights of (E,R,N,K) = (32,16384,2048,4096) in bfloat16 486 us instead of 395, 8192^3 forward 863 instead of 785.)
 template <typename TO, int BM, int BN, int THREADS, int MI, int NI, typename Put>
 __device__ __forceinline__ void emm_store_lines(lds_char* lds, const f4 (&acc)[MI][NI], int rm, int cn, Put put) {
   constexpr int PER = Elem<TO>::PER16, ROW = BN * sizeof(TO);

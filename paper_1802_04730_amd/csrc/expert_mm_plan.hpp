@@ -16,8 +16,8 @@ inline int64_t most_row_tiles(int64_t R, int64_t E, int64_t bm) {
 inline double expected_row_tiles(int64_t R, int64_t E, int64_t bm) { return (double)R / bm + 0.5 * (double)(E < R ? E : R); }
 
 // Side of the (square) tile, `most` or less, for `tiles(side)` tiles: the estimate is a compute unit's number of tiles times a
-// tile's products, over the rate that the side reaches on large extents (relative to 256; 16-bit storage, 8192^3: 1268, 1092 TFLOP/s
-// and about 780).  Larger tiles read less per product; smaller ones lose less to the last row tile of an expert and to compute units
+// tile's products, over the rate that the side reaches on large extents (relative to 256, all before tiles were stored by whole lines; 16-bit
+// storage, 8192^3: 1268, 1092 TFLOP/s and about 780).  Larger tiles read less per product; smaller ones lose less to the last row tile of an expert and to compute units
 // without a tile.  Measured, us, sides 256 / 128 / 64: (E,R,N,K) = (8,16384,4096,4096) 492 / 617 / -, (16,8192,4096,2048) 195 / 192 / 266,
 // (16,2048,2048,2048) 51 / 36 / 41, (4,2000,512,512) 21 / 12 / 8.  fp32 takes 64 always: at a rate of the matrix core that is a sixteenth, no tile is
 // short of operands ((16,2048,2048,2048) 497 / 259 / 223, (64,16384,1024,2048) 1023 / 777 / 692); products with an operand across its rows
@@ -45,7 +45,7 @@ int expert_tile_side(int most, int cus, F tiles) {
 // the longest expert's rows take their time however many compute units wait.  Estimated, us: rounds of workgroups (two on a compute unit) times
 // the rows of a part of the longest expert, taken as twice the average, plus, with parts, a launch and the way of the partial sums
 // to the workspace and back; more parts where they save 15 %.  Measured, us, one part / chosen: bfloat16 (E,R,N,K) = (4,65536,256,256)
-// 164 / 40 (8 parts), (1,8192,512,512) 63 / 21 (8); fp32 (4,65536,256,256) 514 / 125 (8), (2,3000,64,64) 42 / 17 (16).
+// 164 / 38 (8 parts), (1,8192,512,512) 60 / 23 (8); fp32 (4,65536,256,256) 521 / 124 (8), (2,3000,64,64) 42 / 10 (16).
 constexpr int EMM_MOST_PARTS = 16;
 inline int expert_weights_parts(bool f32, int cus, int64_t R, int64_t E, int64_t N, int64_t K, int side) {
   const double tiles = (double)E * ceil_div(N, side) * ceil_div(K, side), rows = (double)R / E * (E > 1 ? 2 : 1);
