@@ -21,8 +21,8 @@
 //
 // Measured, bfloat16: one matrix of 8192^3 785 us forward (1400 TFLOP/s, tile of 256), 1024 dX, 1081 dW (128); 32 experts of 512 rows each, N = 2048,
 // K = 4096: 282, 375, 382 us; of uneven shares 369-410, 360-413, 389-404: the last round of tiles, and last rows of experts, are
-// not full.  fp32, 2100 rows of 12 experts, 1001 x 517: 40, 50, 44 us.  Tried and left: two stages with all fragments read at once, four
-// stages of 64 bytes (404 us forward at uneven shares where two of 128 took 352), 16 wavefronts a tile of 256 (spills), tiles of 256 x 128
+// not full.  fp32, 2100 rows of 12 experts, 1001 x 517: 40, 50, 44 us.  Tried and left: two stages with all fragments read at once
+// (uneven shares: 352, 538, 729 us, by spills), four stages of 64 bytes (404, 411, 539), 16 wavefronts a tile of 256 (spills), tiles of 256 x 128
 // in a ring of three (1088 TFLOP/s at 8192^3 where this then reached 1268, more lost at ragged ends), the last round's tiles shared by two
 // workgroups, and the next tile's first stages requested before this one is stored (no gain).
 #pragma once
