@@ -495,7 +495,7 @@ tc_status tc_route_grad(const void *L, const int32_t *Id, const float *dWt,
  * Products grouped by expert, ragged: for the rows r of expert e, Off(e) <= r < Off(e+1),
  *     Y(r,n) = sum_k X(s(r),k) * W(e,n,k)        s(r) = Row(r), or r if Row is NULL
  *     Y(r,n) = fmaxf(Y(r,n), 0)                  if relu
- * X: [T,K] (T = R if Row is NULL)   W: [E,N,K]   Off: [E+1]   Row: [R] or NULL
+ * X: [T,K] (T = R if Row is NULL, unless R is 0)   W: [E,N,K]   Off: [E+1]   Row: [R] or NULL
  * Y: [R,N].  Experts may own any number of rows, none among them.  Rows from Off(E) on (and
  * below Off(0)) belong to no expert: from Off(E) on they are set to 0, below Off(0) not written.  Offsets are
  * clamped to [0, R]; where they decrease, an expert owns nothing.  A Row outside [0, T) is a row of zeros.

@@ -370,7 +370,7 @@ tc_status tc_route_grad(const void* L, const int32_t* Id, const float* dWt, void
 
 tc_status tc_expert_mm(const void* X, const void* W, const int32_t* Off, const int32_t* Row, void* Y, int64_t T, int64_t R, int64_t E, int64_t N, int64_t K,
                        int32_t relu, tc_type type, void* hip_stream) {
-  if (!known(type) || T < 0 || R < 0 || E <= 0 || N <= 0 || K <= 0 || (!Row && T != R)) return TC_ERR_SHAPE;
+  if (!known(type) || T < 0 || R < 0 || E <= 0 || N <= 0 || K <= 0 || (R && !Row && T != R)) return TC_ERR_SHAPE;
   if (!W || !Off || (R && (!Y || (T && !X)))) return TC_ERR_NULL;
   if (R && (Y == X || Y == W || Y == static_cast<const void*>(Off) || Y == static_cast<const void*>(Row))) return TC_ERR_ALIAS;
   if (misaligned(X) || misaligned(W) || misaligned(Off) || misaligned(Row) || misaligned(Y)) return TC_ERR_ALIGN;
@@ -407,7 +407,7 @@ size_t tc_expert_mm_grad_w_workspace_bytes(int64_t R, int64_t E, int64_t N, int6
 
 tc_status tc_expert_mm_grad_w(const void* dY, const void* X, const int32_t* Off, const int32_t* Row, void* dW, int64_t T, int64_t R, int64_t E, int64_t N,
                               int64_t K, int32_t add, tc_type type, tc_type grad_type, void* workspace, size_t workspace_bytes, void* hip_stream) {
-  if (!known(type) || (grad_type != type && grad_type != TC_F32) || T < 0 || R < 0 || E <= 0 || N <= 0 || K <= 0 || (!Row && T != R)) return TC_ERR_SHAPE;
+  if (!known(type) || (grad_type != type && grad_type != TC_F32) || T < 0 || R < 0 || E <= 0 || N <= 0 || K <= 0 || (R && !Row && T != R)) return TC_ERR_SHAPE;
   if (!Off || !dW || (R && (!dY || (T && !X)))) return TC_ERR_NULL;
   if (dW == dY || dW == X || dW == static_cast<const void*>(Off) || dW == static_cast<const void*>(Row)) return TC_ERR_ALIAS;
   if (workspace && (workspace == dY || workspace == X || workspace == dW || workspace == static_cast<const void*>(Off) || workspace == static_cast<const void*>(Row)))

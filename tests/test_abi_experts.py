@@ -138,3 +138,13 @@ def test_nothing_is_thrown_at_extremes(L):
             if s[at] > (1 << 31):
                 assert L.tc_embed(A, B, C, *s, 1.0, F32, None) == UNSUPPORTED
     assert isinstance(ctypes.c_int(L.tc355_version()).value, int)
+
+
+def test_an_empty_list_of_rows_may_be_null(L):
+    """A step without routed rows: a list of no elements comes as NULL, as an array without elements does, whatever X holds."""
+    for T in (0, 4):
+        for row in (None, D):
+            assert L.tc_expert_mm(A, B, C, row, None, T, 0, 3, 8, 8, 0, BF16, None) == OK
+            assert L.tc_expert_mm_grad_w(None, A, C, row, E_, T, 0, 3, 8, 8, 1, BF16, F32, None, 0, None) == OK
+    assert L.tc_expert_mm(A, B, C, None, E_, 4, 6, 3, 8, 8, 0, BF16, None) == SHAPE  # (with rows, T is R without a list)
+    assert L.tc_expert_mm_grad_w(A, B, C, None, E_, 4, 6, 3, 8, 8, 1, BF16, F32, None, 0, None) == SHAPE

@@ -542,3 +542,16 @@ def test_refusals_of_the_binding():
         tc.tc_expert_sum(f(6, 8), f(3, 2), i(3, 3), f(3, 8))
     with pytest.raises(ValueError):
         tc.tc_expert_sum_grad(f(3, 8), f(6, 8), f(3, 2), i(3, 2), f(5, 8), f(3, 2))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_products_of_no_routed_rows(dtype):
+    """Tokens, but no rows: an empty list, which has no address."""
+    X, W, off, row = _rand((5, 16), dtype, 1), _rand((3, 8, 16), dtype, 2), _ints([0, 0, 0, 0]), _ints([])
+    none = torch.empty((0, 8), dtype=dtype, device="cuda")
+    tc.tc_expert_mm(X, W, off, row, none)
+    for grad in {dtype, torch.float32}:
+        for add in (False, True):
+            dW = torch.full((3, 8, 16), 3.0, dtype=grad, device="cuda")
+            tc.tc_expert_mm_grad_w(none, X, off, row, dW, add=add)
+            assert bool((dW == (3.0 if add else 0.0)).all())
