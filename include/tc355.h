@@ -498,7 +498,8 @@ tc_status tc_route_grad(const void *L, const int32_t *Id, const float *dWt,
  * X: [T,K] (T = R if Row is NULL, unless R is 0)   W: [E,N,K]   Off: [E+1]   Row: [R] or NULL
  * Y: [R,N].  Experts may own any number of rows, none among them.  Rows from Off(E) on (and
  * below Off(0)) belong to no expert: from Off(E) on they are set to 0, below Off(0) not written.  Offsets are
- * clamped to [0, R]; where they decrease, an expert owns nothing.  A Row outside [0, T) is a row of zeros.
+ * clamped to [0, R], and one below an earlier one counts as that one: where they decrease, an expert owns
+ * nothing, and no row has two experts.  A Row outside [0, T) is a row of zeros.
  * An fp32 sum over k is taken on the matrix core in blocks; NaN and Inf stay in the
  * rows and columns that read them.  The clamp maps NaN and -0 to +0.
  */

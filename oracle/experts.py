@@ -83,8 +83,8 @@ def _source(X, Row, r):
 
 
 def _experts(Off, R):
-    """(expert, its rows), rows clamped to [0, R)."""
-    at = np.clip(Off, 0, R)
+    """(expert, its rows): offsets clamped to [0, R], and from where they decrease on as they were, so that no row has two experts."""
+    at = np.maximum.accumulate(np.clip(Off, 0, R))
     return [(e, range(at[e], at[e + 1])) for e in range(len(Off) - 1)]
 
 

@@ -70,3 +70,10 @@ def test_the_chosen_tile_is_never_larger_than_asked_for(plans):
         for most in (64, 128, 256):
             assert plans.rows_side(most, CUS, R, E, N) in (64, 128, 256)
             assert plans.rows_side(most, CUS, R, E, N) <= most
+
+
+def test_offsets_that_decrease_are_tried_on_every_large_kernel(plans):
+    (R, E, N, K), (R2, E2, N2, K2), (R3, E3, N3, K3) = big.DECREASING
+    assert plans.rows_side(256, CUS, R, E, N) == 256
+    assert plans.rows_side(128, CUS, R2, E2, K2) == 128
+    assert plans.weights_parts(0, CUS, R3, E3, N3, K3, plans.weights_side(128, CUS, E3, N3, K3)) > 1

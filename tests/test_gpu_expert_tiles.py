@@ -159,3 +159,24 @@ def test_results_beyond_the_type_and_far_below_one(dtype):
         want = (X.double() @ W[0].double().t()).float().to(dtype)
         assert torch.equal(Y, want) or bool(((Y.double() - want.double()).abs() <= 2 * UNIT[dtype] * want.double().abs()).all())
         assert bool(torch.isinf(Y).all()) == (value == big)
+
+
+# R, E, N, K: tiles of 256 forward, tiles of 128 for dX, rows cut into parts for dW
+DECREASING = [(4100, 3, 3600, 200), (4100, 3, 200, 3600), (3000, 3, 64, 64)]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_offsets_that_decrease_on_large_tiles_and_in_parts(dtype):
+    """An offset below an earlier one counts as that one."""
+    for R, E, N, K in DECREASING:
+        raw = [0, R - 700, R // 3, R - 100]
+        off = np.maximum.accumulate(raw)
+        X, W, dY = _rand((R, K), dtype, 1), _rand((E, N, K), dtype, 2, K ** -0.5), _rand((R, N), dtype, 3)
+        Y, dX, dW = (torch.full_like(t, float("nan")) for t in (dY, X, W))
+        tc.tc_expert_mm(X, W, _ints(raw), None, Y)
+        tc.tc_expert_mm_grad_x(dY, W, _ints(raw), None, dX)
+        tc.tc_expert_mm_grad_w(dY, X, _ints(raw), None, dW, _bytes(tc.tc_expert_mm_grad_w_workspace_bytes(R, E, N, K)))
+        x, w, d = X.double(), W.double(), dY.double()
+        _close(Y, *_by_expert(off, R, N, lambda e, a, b: (x[a:b] @ w[e].t(), x[a:b].abs() @ w[e].abs().t())), K, dtype)
+        _close(dX, *_by_expert(off, R, K, lambda e, a, b: (d[a:b] @ w[e], d[a:b].abs() @ w[e].abs())), N, dtype)
+        _close(dW, *_weights(d, x, off, None), R, dtype)

@@ -555,3 +555,27 @@ def test_products_of_no_routed_rows(dtype):
             dW = torch.full((3, 8, 16), 3.0, dtype=grad, device="cuda")
             tc.tc_expert_mm_grad_w(none, X, off, row, dW, add=add)
             assert bool((dW == (3.0 if add else 0.0)).all())
+
+
+DECREASING = [(70, 3, [0, 50, 20, 500]), (70, 3, [5, 4, 3, 2]), (70, 3, [2 ** 31 - 1, -2 ** 31, 0, 70]), (300, 4, [0, 200, 10, 250, 100]), (600, 2, [400, 0, 500]),
+              (90, 130, [(37 * e) % 101 for e in range(131)]), (400, 64, [300 if e == 3 else 5 * e for e in range(65)]), (700, 200, [3 * e if e % 70 else 600 - e for e in range(201)])]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("R,E,Off", DECREASING)
+def test_offsets_that_decrease_give_no_row_to_two_experts(dtype, R, E, Off):
+    """An offset below an earlier one counts as that one, in all three products, and the rows before the first one are left alone."""
+    N, K = 72, 40
+    Off = np.array(Off)
+    X, W, dY = _rand((R, K), dtype, 1), _rand((E, N, K), dtype, 2), _rand((R, N), dtype, 3)
+    first = int(np.clip(Off[0], 0, R))
+    for _ in range(2):
+        Y, dX = (torch.full((R, n), 7.0, dtype=dtype, device="cuda") for n in (N, K))
+        dW = torch.full((E, N, K), float("nan"), dtype=dtype, device="cuda")
+        tc.tc_expert_mm(X, W, _ints(Off), None, Y)
+        tc.tc_expert_mm_grad_x(dY, W, _ints(Off), None, dX)
+        tc.tc_expert_mm_grad_w(dY, X, _ints(Off), None, dW)
+        for got, (want, mag), n in ((Y, ref.expert_mm(_np(X), _np(W), Off, None, R, False), K), (dX, ref.expert_mm_grad_x(_np(dY), _np(W), Off, None), N)):
+            want[:first] = 7.0
+            _close(got, want, mag, n, dtype)
+        _close(dW, *ref.expert_mm_grad_w(_np(dY), _np(X), Off, None), R, dtype)
