@@ -41,6 +41,20 @@ int expert_tile_side(int most, int cus, F tiles) {
   return best;
 }
 
+// Whether a product whose experts have fewer than 64 rows on average goes to the kernel for few rows (expert_rows.hpp: 16 rows by 32 columns, no
+// LDS) rather than to tiles.  Either one's time grows with its workgroups per compute unit beyond a half; a lone tile takes 4.5 times (rows of no
+// whole 16-byte pieces: twice, fp32: 5 and 4.5 times) as long as a lone workgroup of the few rows.  Measured, us, few rows / tiles, weights from memory: bfloat16, 8 experts, N = 4096,
+// K = 2048, with 4 rows each 30 / 35, 8: 32 / 35, 16: 42 / 35, 32: 61 / 35, 63: 103 / 40 (64 rows of one expert, in a kernel of that shape that was here: 67);
+// 32 experts, 2048, 1024: 4 rows 30 / 26; small products always: 12 experts of 58 rows, 130, 1000: 7.4 / 10.2; fp32, 8 experts, 2048, 1024: 16 rows 19 / 25, 32: 29 / 25;
+// width 4099 x 2047: 4 rows 70 / 58.  Over 2417 shapes of up to 63 rows an expert the choice is 1.5 % off the better one (geometric mean; at worst 1.54 times).
+// Where one expert has all rows, which no average tells: 64 x 32 rows, 1024 x 2048 88 / 20 (tiles are taken), 8 x 8 rows, 4096 x 2048 14 / 17 (few rows).
+inline bool expert_few_rows(bool f32, bool whole, int cus, int64_t R, int64_t E, int64_t N) {
+  if (R / E >= 64) return false;
+  const double few = expected_row_tiles(R, E, 16) * ceil_div(N, 32) / cus, tile = expected_row_tiles(R, E, 64) * ceil_div(N, 64) / cus;
+  const double lone = f32 ? (whole ? 5 : 4.5) : whole ? 4.5 : 2, each = f32 ? 6 : whole ? 1 : 3;
+  return 1 + 1.5 * (few > 0.5 ? few - 0.5 : 0) <= lone + each * (tile > 0.5 ? tile - 0.5 : 0);
+}
+
 // Parts into which the gradient of the weights cuts each expert's rows: tiles of the weights alone may be too few for the device, and
 // the longest expert's rows take their time however many compute units wait.  Estimated, us: rounds of workgroups (two on a compute unit) times
 // the rows of a part of the longest expert, taken as twice the average, plus, with parts, a launch and the way of the partial sums

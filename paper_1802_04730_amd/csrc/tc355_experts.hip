@@ -166,12 +166,12 @@ tc_status launch_rows_tile(ExpertRowsArgs a, hipStream_t s) {
   return launched();
 }
 
-template <typename T, int RT, int CT, int WK>
+template <typename T, int CT, int WK>
 tc_status launch_few_rows(ExpertRowsArgs a, hipStream_t s) {
   a.nt = (int)ceil_div(a.NO, 16 * CT);
-  const int64_t grid = (most_row_tiles(a.R, a.E, 16 * RT) * a.nt + 7) / 8 * 8;
+  const int64_t grid = (most_row_tiles(a.R, a.E, 16) * a.nt + 7) / 8 * 8;
   if (grid > kMostIndex / (64 * WK) * 2) return TC_ERR_UNSUPPORTED;
-  expert_few_rows_kernel<T, RT, CT, WK><<<dim3((unsigned)grid), dim3(64 * WK), 0, s>>>(a);
+  expert_few_rows_kernel<T, CT, WK><<<dim3((unsigned)grid), dim3(64 * WK), 0, s>>>(a);
   return launched();
 }
 
@@ -378,12 +378,8 @@ tc_status tc_expert_mm(const void* X, const void* W, const int32_t* Off, const i
   if (R == 0) return TC_OK;
   const ExpertRowsArgs a{X, W, Y, nullptr, Off, Row, (int)R, (int)T, (int)E, (int)K, (int)N, 0, relu != 0};
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
-  const int64_t share = R / E;
-  if (share < 64)
-    return took("expert_mm:rows", by_type(type, [&](auto t) {
-                  typedef decltype(t) T_;
-                  return share < 16 ? launch_few_rows<T_, 1, 2, 4>(a, s) : launch_few_rows<T_, 4, 2, 4>(a, s);
-                }));
+  if (expert_few_rows(type == TC_F32, K % (type == TC_F32 ? 4 : 8) == 0, compute_units(), R, E, N))
+    return took("expert_mm:rows", by_type(type, [&](auto t) { return launch_few_rows<decltype(t), 2, 4>(a, s); }));
   return took("expert_mm:tile", run_rows<false>(a, type, s));
 }
 
