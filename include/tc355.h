@@ -472,7 +472,8 @@ tc_status tc_embed_grad(const void *dO, const int32_t *Idx, void *dLUT,
  * (norm = 1: if one is among the chosen, which it is).
  * 1 <= k <= E; E <= 1023, k <= 64 and T < 2^28 (TC_ERR_UNSUPPORTED beyond).
  *   workspace  device scratch of at least tc_route_workspace_bytes(...) bytes,
- *              16-byte aligned; NULL where that is 0 (a few tokens).
+ *              16-byte aligned; NULL where that is 0 (a few tokens).  Up to 64 tokens less only
+ *              costs time.
  */
 size_t tc_route_workspace_bytes(int64_t T, int64_t E, int64_t k);
 tc_status tc_route(const void *L, float *Wt, int32_t *Id, int32_t *Off,

@@ -15,6 +15,10 @@
 // all of it is one workgroup's, in one launch.  No atomics on memory; integer ones in LDS.  Measured: 16 tokens of 64 experts, 4
 // chosen, 4.7 us; 16384 of 128, 8 chosen, 12.8 for the selection (29 by exchange through LDS), 4.2 for the sums, 6.3 for the places (63 where every
 // workgroup added the earlier ones' counts up), 9.6 for the gradient.
+// The lines between the forms, us a call: one workgroup / two launches, 64 experts of which 4: 32 tokens 6.3 / 7.9, 48: 7.8 / 8.0, 64: 9.1 / 8.1; 128 of which 8:
+// 9.8 / 11.4, 14.2 / 11.6, 17.2 / 11.8; 256 of which 8: 37 / 39, 55 / 40, 71 / 40; 8 of which 2: 4.8 / 6.4, 5.5 / 6.5, 6.2 / 6.7.
+// Counts added up by every workgroup / by a launch of its own, 512, 1024 and 2048 tokens: 64 experts 9.4 / 11.4, 10.0 / 11.4, 12.2 / 11.7; 128: 13.4 / 15.0,
+// 14.7 / 15.3, 17.5 / 15.6; 256: 42.7 / 43.7, 45.0 / 44.0, 50.9 / 44.6; 8: 7.5 / 9.5, 8.1 / 9.6, 9.5 / 9.6.
 #pragma once
 #include "expert_types.hpp"
 #include "key_sort.hpp"
@@ -22,10 +26,11 @@
 namespace tc355 {
 
 constexpr int ROUTE_TOKENS = 32;      // of a workgroup
-constexpr int ROUTE_ALONE = 64;       // tokens that one workgroup routes by itself
+constexpr int ROUTE_ALONE = 32;       // tokens that one workgroup routes by itself
+constexpr int ROUTE_MOST_ALONE = 64;  // the same without a workspace
 constexpr int ROUTE_MOST_E = 1023;    // (with the empty slots' bin: 10 bits)
 constexpr int ROUTE_MOST_K = 64;
-constexpr int ROUTE_DIRECT_TILES = 16;
+constexpr int ROUTE_DIRECT_TILES = 32;  // up to so many workgroups add the earlier ones' counts up themselves
 
 struct RouteArgs {
   const void* L;  // [T][E]

@@ -329,10 +329,11 @@ tc_status tc_route(const void* L, float* Wt, int32_t* Id, int32_t* Off, int32_t*
   if (misaligned(L)) return TC_ERR_ALIGN;
   if (E > ROUTE_MOST_E || k > ROUTE_MOST_K || prod_reaches({std::max<int64_t>(T, 1), k}, kMostRows) || T >= kMostTokens) return TC_ERR_UNSUPPORTED;
   const int64_t need = route_ws(T, E);
-  if (need && (!workspace || misaligned(workspace) || workspace_bytes < (size_t)need)) return TC_ERR_WORKSPACE;
+  const bool tiles = need && workspace && !misaligned(workspace) && workspace_bytes >= (size_t)need;
+  if (!tiles && T > ROUTE_MOST_ALONE) return TC_ERR_WORKSPACE;
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
-  RouteArgs a{L, Wt, Id, Off, Row, Place, need ? static_cast<int*>(workspace) : nullptr, (int)T, (int)E, (int)k, norm != 0, bits_of(E),
-              need ? (int)ceil_div(T, ROUTE_TOKENS) : 1, 0, need ? ROUTE_TOKENS : ROUTE_ALONE};
+  RouteArgs a{L, Wt, Id, Off, Row, Place, tiles ? static_cast<int*>(workspace) : nullptr, (int)T, (int)E, (int)k, norm != 0, bits_of(E),
+              tiles ? (int)ceil_div(T, ROUTE_TOKENS) : 1, 0, tiles ? ROUTE_TOKENS : ROUTE_MOST_ALONE};
   a.summed = a.tiles > ROUTE_DIRECT_TILES;
   const size_t bins = (size_t)4 << a.bits;
   return by_type(type, [&](auto x) {

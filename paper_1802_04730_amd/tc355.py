@@ -456,7 +456,7 @@ def tc_route_workspace_bytes(T: int, E: int, k: int) -> int:
 def tc_route(L, Wt, Id, Off, Row, Place, workspace=None, norm: bool = False, stream=None) -> None:
     """Weights Wt[T,k] and numbers Id[T,k] of the k largest of L[T,E], and the slots by expert: Off[E+1], Row[T*k], Place[T,k].
 
-    ``workspace``: a uint8 tensor of at least tc_route_workspace_bytes(T, E, k) bytes (None only when that is 0)."""
+    ``workspace``: a uint8 tensor of at least tc_route_workspace_bytes(T, E, k) bytes (None when that is 0; up to 64 tokens less only costs time)."""
     if _FAST is not None:
         status = _FAST.route(_AT["tc_route"], L, Wt, Id, Off, Row, Place, workspace, norm, stream)
         if status >= 0:

@@ -148,3 +148,11 @@ def test_an_empty_list_of_rows_may_be_null(L):
             assert L.tc_expert_mm_grad_w(None, A, C, row, E_, T, 0, 3, 8, 8, 1, BF16, F32, None, 0, None) == OK
     assert L.tc_expert_mm(A, B, C, None, E_, 4, 6, 3, 8, 8, 0, BF16, None) == SHAPE  # (with rows, T is R without a list)
     assert L.tc_expert_mm_grad_w(A, B, C, None, E_, 4, 6, 3, 8, 8, 1, BF16, F32, None, 0, None) == SHAPE
+
+
+def test_the_router_wants_a_workspace_where_two_launches_are_faster(L):
+    size = L.tc_route_workspace_bytes
+    for E, k in ((8, 2), (64, 4), (128, 8), (1023, 64)):
+        assert size(32, E, k) == 0 and size(33, E, k) > 0 and size(64, E, k) > 0
+        grows = [size(T, E, k) for T in range(1, 5000)]
+        assert grows == sorted(grows)

@@ -579,3 +579,19 @@ def test_offsets_that_decrease_give_no_row_to_two_experts(dtype, R, E, Off):
             want[:first] = 7.0
             _close(got, want, mag, n, dtype)
         _close(dW, *ref.expert_mm_grad_w(_np(dY), _np(X), Off, None), R, dtype)
+
+
+@pytest.mark.parametrize("T,E,k", [(32, 64, 4), (33, 64, 4), (48, 8, 2), (64, 128, 8), (64, 300, 17), (63, 1023, 64), (65, 16, 4), (1024, 8, 2), (1025, 8, 2), (700, 40, 3)])
+def test_route_with_and_without_a_workspace(T, E, k):
+    """The same results in one launch and in several, with a workspace and, up to 64 tokens, without one."""
+    L = _logits(T, E, torch.bfloat16, T + E)
+    want = _check_route(L, k, True)
+    assert tc.last_path() == ("route:one" if T <= 32 else "route:tiles")
+    if T <= 64:
+        for ws in (None, _bytes(16)):
+            out = [torch.full_like(w, 77) for w in want]
+            tc.tc_route(L, *out, ws, True)
+            assert tc.last_path() == "route:one" and all(torch.equal(a, b) for a, b in zip(out, want))
+    else:
+        with pytest.raises(tc.TcError):
+            tc.tc_route(L, *want, None, True)
