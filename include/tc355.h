@@ -443,7 +443,8 @@ tc_status tc_embed(const void *LUT, const int32_t *Idx, void *O, int64_t E,
  * token names the row; add = 1: the sum is added to what dLUT holds, and rows that no
  * token names are not touched.
  *   workspace  device scratch of at least tc_embed_grad_workspace_bytes(...)
- *              bytes, 16-byte aligned (may be NULL for T = 0); contents on entry are irrelevant, calls that
+ *              bytes, 16-byte aligned (may be NULL for T = 0); what serves T tokens serves
+ *              fewer; contents on entry are irrelevant, calls that
  *              share it must be ordered on one stream.
  */
 size_t tc_embed_grad_workspace_bytes(int64_t E, int64_t D, int64_t T);

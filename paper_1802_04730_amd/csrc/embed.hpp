@@ -17,8 +17,14 @@
 
 namespace tc355 {
 
-constexpr int EMBED_CHUNK = 32;       // places of a chunk
-constexpr int EMBED_SMALL_CHUNK = 8;  // the same where chunks are few
+// Places of a chunk.  Small ones spread few tokens over the device; long ones hand fewer partial sums on, which counts sooner where the table's rows of
+// zeros keep the device busy anyway.  us, 8 / 32 places, table written: 32000 x 2048 in fp32 of bfloat16, 4000 tokens 70 / 70, 9000: 90 / 85, 16000: 102 / 87;
+// 50000 x 4096 bfloat16 101 / 98, 124 / 109, 142 / 112; 5000 x 256 23 / 30, 38 / 42, 46 / 44.  Added to: 32 / 50, 53 / 65, 69 / 70, 20000: 76 / 74;
+// 37 / 57, 62 / 72, 89 / 79, 109 / 90; 24 / 33, 39 / 44, 46 / 46, 51 / 47.
+constexpr int EMBED_CHUNK = 32;
+constexpr int EMBED_SMALL_CHUNK = 8;
+constexpr int EMBED_FEW_WRITTEN = 8192;  // so many tokens and more take long chunks where the table is written,
+constexpr int EMBED_FEW_ADDED = 14336;   // and where it is added to
 
 struct EmbedArgs {
   const void* LUT;

@@ -17,7 +17,9 @@ constexpr int SORT_THREADS = 512;
 constexpr int SORT_TILE = 2048;             // keys of a workgroup
 constexpr int SORT_ROUNDS = 4;              // keys of a thread
 constexpr int SORT_SMALL = 8192;            // keys that are ranked by counting
-constexpr int SORT_DIRECT_TILES = 32;       // up to so many workgroups add the earlier ones' counts up themselves
+// Up to so many workgroups add the earlier ones' counts up themselves; beyond, a launch of its own does.  us, a whole gradient, without / with that
+// launch: 20000 tokens 74 / 78, 50 / 54, 50000: 130 / 133, 61 / 64, 100000: 235 / 233, 87 / 87 (32000 x 2048, 10007 x 333).
+constexpr int SORT_DIRECT_TILES = 32;
 static_assert(SORT_TILE == SORT_ROUNDS * SORT_THREADS, "keys of a workgroup");
 
 // Lanes of the wavefront that have the same digit (of `bits` bits) as this one, among `on`.

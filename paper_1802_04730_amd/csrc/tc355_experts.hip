@@ -62,8 +62,8 @@ RowLanes row_lanes(int64_t width, int per16) {
 // ---- token tables -----------------------------------------------------------------------------------------------------------
 
 struct EmbedGradPlan {
-  int key_bits, passes, bits, chunk;
-  int64_t tiles, chunks;
+  int key_bits, passes, bits;
+  int64_t tiles;
   int64_t key_a, order_a, key_b, order_b, count, part, bytes;  // offsets into the workspace
 };
 
@@ -73,8 +73,8 @@ EmbedGradPlan embed_grad_plan(int64_t E, int64_t D, int64_t T) {
   p.passes = (int)ceil_div(p.key_bits, SORT_MOST_BITS);
   p.bits = (int)ceil_div(p.key_bits, p.passes);
   p.tiles = ceil_div(T, SORT_TILE);
-  p.chunk = T < 512 * EMBED_CHUNK ? EMBED_SMALL_CHUNK : EMBED_CHUNK;
-  p.chunks = ceil_div(T, p.chunk);
+  // (as many as a table that is added to has; never fewer than fewer tokens have: a workspace for more tokens serves fewer)
+  const int64_t chunks = std::max(ceil_div(T, EMBED_CHUNK), ceil_div(std::min<int64_t>(T, EMBED_FEW_ADDED), EMBED_SMALL_CHUNK));
   int64_t at = 0;
   const auto take = [&](int64_t n) {
     const int64_t o = at;
@@ -88,7 +88,7 @@ EmbedGradPlan embed_grad_plan(int64_t E, int64_t D, int64_t T) {
     p.order_b = take(T * 4);
     p.count = take((p.tiles + 1) * ((int64_t)4 << p.bits));
   }
-  p.part = take(p.chunks * 2 * D * 8);
+  p.part = take(chunks * 2 * D * 8);
   p.bytes = at;
   return p;
 }
@@ -282,10 +282,12 @@ tc_status tc_embed_grad(const void* dO, const int32_t* Idx, void* dLUT, int64_t 
     constexpr int V = decltype(v)::value;
     EmbedGradArgs a{};
     a.dO = dO; a.dLUT = dLUT; a.part = T ? ws + pl.part : nullptr;
-    a.T = (int)T; a.E = (int)E; a.D = (int)D; a.scale = scale; a.add = add != 0; a.chunk = pl.chunk;
+    a.T = (int)T; a.E = (int)E; a.D = (int)D; a.scale = scale; a.add = add != 0;
+    a.chunk = T < (add ? EMBED_FEW_ADDED : EMBED_FEW_WRITTEN) ? EMBED_SMALL_CHUNK : EMBED_CHUNK;
+    const int64_t chunks = ceil_div(T, a.chunk);
     a.lpr = 1;
     while (a.lpr < ceil_div(D, V) && a.lpr < WG_THREADS) a.lpr *= 2;
-    a.token_wgs = (unsigned)ceil_div(pl.chunks, WG_THREADS / a.lpr);
+    a.token_wgs = (unsigned)ceil_div(chunks, WG_THREADS / a.lpr);
     int64_t rows = EMBED_FILL_ROWS;
     while (ceil_div(E, rows) > (int64_t)1 << 22) rows *= 2;  // (fewer than 2^32 threads)
     a.rows = (int)rows;
@@ -297,8 +299,8 @@ tc_status tc_embed_grad(const void* dO, const int32_t* Idx, void* dLUT, int64_t 
     }
     const size_t lds = (size_t)(WG_THREADS / a.lpr) * (2 * a.chunk + 4) * 4;
     embed_grad_kernel<X, Y, V><<<dim3((unsigned)grid), dim3(WG_THREADS), lds, s>>>(a);
-    if (pl.chunks > 1) {
-      const dim3 join((unsigned)ceil_div(pl.chunks, WAVES_PER_WG), (unsigned)std::min<int64_t>(64, ceil_div(ceil_div(D, V), 64)));
+    if (chunks > 1) {
+      const dim3 join((unsigned)ceil_div(chunks, WAVES_PER_WG), (unsigned)std::min<int64_t>(64, ceil_div(ceil_div(D, V), 64)));
       embed_join_kernel<X, Y, V><<<join, dim3(WG_THREADS), 0, s>>>(a);
     }
     return took(T <= SORT_SMALL ? "embed_grad:ranks" : "embed_grad:sort", launched());

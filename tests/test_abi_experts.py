@@ -156,3 +156,12 @@ def test_the_router_wants_a_workspace_where_two_launches_are_faster(L):
         assert size(32, E, k) == 0 and size(33, E, k) > 0 and size(64, E, k) > 0
         grows = [size(T, E, k) for T in range(1, 5000)]
         assert grows == sorted(grows)
+
+
+def test_a_workspace_for_more_tokens_serves_fewer(L):
+    """A program that asks for its largest batch's bytes once is not refused a smaller one."""
+    size = L.tc_embed_grad_workspace_bytes
+    for E, D in ((100, 1), (50000, 333), (1 << 20, 4096)):
+        T = sorted({x for n in (8, 32, 1000, 2048, 8192, 14336, 16384, 57344, 65536, 1 << 20) for x in range(n - 33, n + 34) if x > 0})
+        sizes = [size(E, D, t) for t in T]
+        assert sizes == sorted(sizes) and sizes[0] > 0
