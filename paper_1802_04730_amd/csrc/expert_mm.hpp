@@ -122,8 +122,8 @@ __device__ __forceinline__ bool expert_tile(const int* off, int E, int R, int bm
   return false;
 }
 
-// The first row of expert e: the most of Off(0..e).  (A trip to memory beside that of the expert's own: dW of 32 rows of 8 experts, 4096 x 2048, 28.9
-// us where 28.1 without, of 8192 rows of 128 experts, 512 x 1024, 36.3 and 35.7.)
+// The first row of expert e: the most of Off(0..e).  (A trip to memory beside that of the expert's own: dW of 32 rows of 8 experts, 4096 x 2048, 29.2
+// us where 28.2 without, of 8020 rows of 64, 2672 x 1824, 202 and 196, of 16384 rows of 32, 2048 x 4096, 353 and 352.  Asked for before the expert is known: no faster.)
 __device__ __forceinline__ int expert_first_row(const int* off, int e, int R) {
   const int lane = threadIdx.x & 63, own = offset_within(off, e, R);
   int most = 0;

@@ -16,12 +16,13 @@ inline int64_t most_row_tiles(int64_t R, int64_t E, int64_t bm) {
 inline double expected_row_tiles(int64_t R, int64_t E, int64_t bm) { return (double)R / bm + 0.5 * (double)(E < R ? E : R); }
 
 // Side of the (square) tile, `most` or less, for `tiles(side)` tiles: the estimate is a compute unit's number of tiles times a
-// tile's products, over the rate that the side reaches on large extents (relative to 256, all before tiles were stored by whole lines; 16-bit
-// storage, 8192^3: 1268, 1092 TFLOP/s and about 780).  Larger tiles read less per product; smaller ones lose less to the last row tile of an expert and to compute units
-// without a tile.  Measured, us, sides 256 / 128 / 64: (E,R,N,K) = (8,16384,4096,4096) 492 / 617 / -, (16,8192,4096,2048) 195 / 192 / 266,
-// (16,2048,2048,2048) 51 / 36 / 41, (4,2000,512,512) 21 / 12 / 8.  fp32 takes 64 always: at a rate of the matrix core that is a sixteenth, no tile is
-// short of operands ((16,2048,2048,2048) 497 / 259 / 223, (64,16384,1024,2048) 1023 / 777 / 692); products with an operand across its rows
-// take 128 at most, since 256 has too few registers left for them (dX and dW of (8,16384,4096,4096): 557 and 856 / 613 and 618).
+// tile's products, over the rate that the side reaches relative to 256.  Larger tiles read less per product; smaller ones lose less to the last row tile of an
+// expert and to compute units without a tile.  Measured, bfloat16, us, sides 256 / 128 / 64: 8192^3 774 / 975 / 1468; uneven shares, (E,R,N,K) = (8,16384,4096,4096) 508 / 603 / 910,
+// (16,8192,4096,2048) 181 / 175 / 249, (32,16384,2048,4096) 349 / 352 / 493, (16,2048,2048,2048) 46 / 31 / 40, (4,2000,512,512) 15.6 / 7.5 / 6.2.  Over 70 drawn shapes the choice is
+// 2.0 % off the best side forward, 0.6 % for dX, 1.1 % for dW (geometric means; at worst 1.35, 1.13, 1.64 times).  fp32 takes 64 always: at a rate of the matrix core that is a
+// sixteenth, no tile is short of operands ((16,2048,2048,2048) 497 / 259 / 223, (64,16384,1024,2048) 1023 / 777 / 692).  Products with an operand across its rows
+// take 128 at most, since there is no tile of 256 for them: one that was tried took 557 us for dX of (8,16384,4096,4096) where 128 took 613, and 856 for dW where
+// 128 took 618 (too few registers).
 template <typename F>
 int expert_tile_side(int most, int cus, F tiles) {
   const struct {
@@ -56,18 +57,20 @@ inline bool expert_few_rows(bool f32, bool whole, int cus, int64_t R, int64_t E,
 }
 
 // Parts into which the gradient of the weights cuts each expert's rows: tiles of the weights alone may be too few for the device, and
-// the longest expert's rows take their time however many compute units wait.  Estimated, us: rounds of workgroups (two on a compute unit) times
-// the rows of a part of the longest expert, taken as twice the average, plus, with parts, a launch and the way of the partial sums
-// to the workspace and back; more parts where they save 15 %.  Measured, us, one part / chosen: bfloat16 (E,R,N,K) = (4,65536,256,256)
-// 164 / 38 (8 parts), (1,8192,512,512) 60 / 23 (8); fp32 (4,65536,256,256) 521 / 124 (8), (2,3000,64,64) 42 / 10 (16).
+// the longest expert's rows take their time however many compute units wait.  Estimated, us: rounds of workgroups (four on a compute unit) times
+// the rows of a part of a longer expert, taken as 1.5 times the average, plus, with parts, a launch and the way of the partial sums
+// to the workspace and back; more parts where they save 15 %.  Measured, us, 1 / 2 / 4 / 8 / 16 parts: bfloat16 (E,R,N,K) = (4,65536,256,256)
+// 161 / 91 / 51 / 37 / 42, (1,8192,512,512) 59 / 36 / 22 / 18 / 22, (4,131072,1024,1024) 634 / 449 / 403 / 397 / 425, (16,16384,256,512) 23 / 25 / 28 / 37 / 54; fp32
+// (4,65536,256,256) 512 / 261 / 136 / 114 / 113, (2,3000,64,64) 41 / 25 / 15 / 10 / 9, (8,8192,1024,512) 93 / 103 / 102 / 114 / 168.  Over 380 shapes the choice is 1.0 % off the best number
+// (geometric mean; at worst 1.28 times).
 constexpr int EMM_MOST_PARTS = 16;
 inline int expert_weights_parts(bool f32, int cus, int64_t R, int64_t E, int64_t N, int64_t K, int side) {
-  const double tiles = (double)E * ceil_div(N, side) * ceil_div(K, side), rows = (double)R / E * (E > 1 ? 2 : 1);
-  const double row = side == 128 ? 0.6 / 64 : f32 ? 0.8 / 32 : 0.25 / 64;  // of a tile, us
+  const double tiles = (double)E * ceil_div(N, side) * ceil_div(K, side), rows = (double)R / E * (E > 1 ? 1.5 : 1);
+  const double row = side == 128 ? 0.5 / 64 : f32 ? 1.0 / 32 : 0.85 / 64;  // of a tile, us
   int best = 1;
   double least = 0;
   for (int s = 1; s <= EMM_MOST_PARTS; s *= 2) {
-    const double t = std::ceil(tiles * s / (2 * cus)) * (rows / s * row + 3) + (s > 1 ? 5 + 8.0 * s * E * N * K / 4e6 : 0);
+    const double t = std::ceil(tiles * s / (4 * cus)) * (rows / s * row + 2) + (s > 1 ? 3.5 + 12.0 * s * E * N * K / 4e6 : 0);
     if (s == 1 || t < 0.85 * least) {
       best = s;
       least = t;
