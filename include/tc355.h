@@ -417,7 +417,8 @@ tc_status tc_lut(int32_t n_tables, const float *const *LUT,
  *  - Every result is the same each time: no sum depends on the order in which
  *    workgroups run.
  *  - Extents below 2^30 (rows of a table: below 2^31 - 1; N and K of the
- *    products: below 2^22); tensors may hold more than 2^31 elements.
+ *    products: below 2^22); tensors may hold more than 2^31 elements.  A product of
+ *    more than 2^24 tiles (64 x 64 and more, each expert's for itself) is TC_ERR_UNSUPPORTED.
  *  - A pointer to an array without elements may be NULL.
  *  - Indices and offsets live on the device, so the host cannot reject them.  Whatever they hold, nothing
  *    outside the named arrays is read or written.

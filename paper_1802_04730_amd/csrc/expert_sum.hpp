@@ -23,9 +23,9 @@ struct ExpertSumArgs {
 };
 
 template <typename T, int V, int SLOTS>
-__global__ __launch_bounds__(WG_THREADS) void expert_sum_kernel(ExpertSumArgs p) {
+__global__ __launch_bounds__(WG_THREADS) void expert_sum_kernel(ExpertSumArgs p, int64_t first) {
   typedef typename Wide<T>::type S;
-  const int64_t g = ((int64_t)blockIdx.x * WG_THREADS + threadIdx.x) / p.lpr;
+  const int64_t g = ((first + blockIdx.x) * WG_THREADS + threadIdx.x) / p.lpr;
   const int64_t t = g / p.cols;
   const RowUnit<V> u((g % p.cols) * p.lpr + (threadIdx.x & (p.lpr - 1)), p.N);
   if (t >= p.T || !u.on) return;
@@ -69,10 +69,10 @@ struct ExpertSumGradArgs {
 };
 
 template <typename T, int V, int SLOTS>
-__global__ __launch_bounds__(WG_THREADS) void expert_sum_grad_kernel(ExpertSumGradArgs p) {
+__global__ __launch_bounds__(WG_THREADS) void expert_sum_grad_kernel(ExpertSumGradArgs p, int64_t first) {
   typedef typename Wide<T>::type S;
   const int lane = threadIdx.x & 63;
-  const int64_t t = (int64_t)blockIdx.x * WAVES_PER_WG + (threadIdx.x >> 6);
+  const int64_t t = (first + blockIdx.x) * WAVES_PER_WG + (threadIdx.x >> 6);
   if (t >= p.T) return;
   const T* dO = static_cast<const T*>(p.dO) + t * p.N;
   if (p.R == 0) {

@@ -230,9 +230,9 @@ struct RouteGradArgs {
 };
 
 template <typename T, int G, int V>
-__global__ __launch_bounds__(WG_THREADS) void route_grad_kernel(RouteGradArgs p) {
+__global__ __launch_bounds__(WG_THREADS) void route_grad_kernel(RouteGradArgs p, int64_t first) {
   const int lane = threadIdx.x & (G - 1);
-  const int64_t t = (int64_t)blockIdx.x * (WG_THREADS / G) + threadIdx.x / G;
+  const int64_t t = (first + blockIdx.x) * (WG_THREADS / G) + threadIdx.x / G;
   if (t >= p.T) return;
   const T* L = static_cast<const T*>(p.L) + t * p.E;
   float x[V], g[V];

@@ -48,6 +48,17 @@ tc_status by_type(tc_type t, F f) {
   return f(f16{});
 }
 
+// launch(workgroups, first): one after the other until all `n` workgroups of WG_THREADS have run.
+template <typename F>
+tc_status in_launches(int64_t n, F launch) {
+  for (int64_t at = 0; at < n;) {
+    const int64_t some = next_launch(n - at, WG_THREADS);
+    launch(dim3((unsigned)some), at);
+    at += some;
+  }
+  return launched();
+}
+
 // Lanes that share a row of `units` 16-byte units, and groups of them that a row takes.
 struct RowLanes {
   int lpr, cols;
@@ -247,14 +258,10 @@ tc_status tc_embed(const void* LUT, const int32_t* Idx, void* O, int64_t E, int6
                 const int v = D < V ? 1 : V;
                 const RowLanes rl = row_lanes(D, v);
                 const EmbedArgs a{LUT, Idx, O, E, T, (int)D, rl.lpr, rl.cols, scale};
-                const int64_t all = ceil_div(T * a.cols, WG_THREADS / a.lpr);
-                for (int64_t at = 0; at < all;) {
-                  const int64_t n = next_launch(all - at, WG_THREADS);
-                  if (v == V) embed_kernel<X, V><<<dim3((unsigned)n), dim3(WG_THREADS), 0, s>>>(a, at);
-                  else embed_kernel<X, 1><<<dim3((unsigned)n), dim3(WG_THREADS), 0, s>>>(a, at);
-                  at += n;
-                }
-                return launched();
+                return in_launches(ceil_div(T * a.cols, WG_THREADS / a.lpr), [&](dim3 n, int64_t at) {
+                  if (v == V) embed_kernel<X, V><<<n, dim3(WG_THREADS), 0, s>>>(a, at);
+                  else embed_kernel<X, 1><<<n, dim3(WG_THREADS), 0, s>>>(a, at);
+                });
               }));
 }
 
@@ -363,10 +370,9 @@ tc_status tc_route_grad(const void* L, const int32_t* Id, const float* dWt, void
   return by_type(type, [&](auto x) {
     return by_lanes(E, 1, [&](auto g, auto v) {
       typedef decltype(x) X;
-      const int64_t grid = ceil_div(T, WG_THREADS / g.value);
-      if (grid > kMostIndex / WG_THREADS * 2) return TC_ERR_UNSUPPORTED;
-      route_grad_kernel<X, g.value, v.value><<<dim3((unsigned)grid), dim3(WG_THREADS), 0, s>>>(a);
-      return took("route_grad:rows", launched());
+      return took("route_grad:rows", in_launches(ceil_div(T, WG_THREADS / g.value), [&](dim3 n, int64_t at) {
+                    route_grad_kernel<X, g.value, v.value><<<n, dim3(WG_THREADS), 0, s>>>(a, at);
+                  }));
     });
   });
 }
@@ -450,16 +456,15 @@ tc_status tc_expert_sum(const void* Y, const float* Wt, const int32_t* Place, vo
                 constexpr int V = Elem<X>::PER16;
                 const RowLanes rl = row_lanes(N, N < V ? 1 : V);
                 const ExpertSumArgs a{Y, Wt, Place, O, T, R, (int)N, (int)k, rl.lpr, rl.cols};
-                const int64_t grid = ceil_div(T * a.cols, WG_THREADS / a.lpr);
-                if (grid > kMostIndex / WG_THREADS * 2) return TC_ERR_UNSUPPORTED;
-                const dim3 g((unsigned)grid), b(WG_THREADS);
                 hipStream_t s = static_cast<hipStream_t>(hip_stream);
-                if (N < V) expert_sum_kernel<X, 1, 4><<<g, b, 0, s>>>(a);
-                else if (k == 1) expert_sum_kernel<X, V, 1><<<g, b, 0, s>>>(a);
-                else if (k == 2) expert_sum_kernel<X, V, 2><<<g, b, 0, s>>>(a);
-                else if (k <= 4) expert_sum_kernel<X, V, 4><<<g, b, 0, s>>>(a);
-                else expert_sum_kernel<X, V, 8><<<g, b, 0, s>>>(a);
-                return launched();
+                return in_launches(ceil_div(T * a.cols, WG_THREADS / a.lpr), [&](dim3 n, int64_t at) {
+                  const dim3 b(WG_THREADS);
+                  if (N < V) expert_sum_kernel<X, 1, 4><<<n, b, 0, s>>>(a, at);
+                  else if (k == 1) expert_sum_kernel<X, V, 1><<<n, b, 0, s>>>(a, at);
+                  else if (k == 2) expert_sum_kernel<X, V, 2><<<n, b, 0, s>>>(a, at);
+                  else if (k <= 4) expert_sum_kernel<X, V, 4><<<n, b, 0, s>>>(a, at);
+                  else expert_sum_kernel<X, V, 8><<<n, b, 0, s>>>(a, at);
+                });
               }));
 }
 
@@ -479,16 +484,15 @@ tc_status tc_expert_sum_grad(const void* dO, const void* Y, const float* Wt, con
   return took("expert_sum_grad:rows", by_type(type, [&](auto x) {
                 typedef decltype(x) X;
                 const ExpertSumGradArgs a{dO, Y, Wt, Place, dY, dWt, T, R, (int)N, (int)k};
-                const int64_t grid = ceil_div(T, WAVES_PER_WG);
-                if (grid > kMostIndex / WG_THREADS * 2) return TC_ERR_UNSUPPORTED;
-                const dim3 g((unsigned)grid), b(WG_THREADS);
                 hipStream_t s = static_cast<hipStream_t>(hip_stream);
                 constexpr int V = Elem<X>::PER16;
-                if (N < V) expert_sum_grad_kernel<X, 1, 4><<<g, b, 0, s>>>(a);
-                else if (k <= 2) expert_sum_grad_kernel<X, V, 2><<<g, b, 0, s>>>(a);
-                else if (k <= 4) expert_sum_grad_kernel<X, V, 4><<<g, b, 0, s>>>(a);
-                else expert_sum_grad_kernel<X, V, 8><<<g, b, 0, s>>>(a);
-                return launched();
+                return in_launches(ceil_div(T, WAVES_PER_WG), [&](dim3 n, int64_t at) {
+                  const dim3 b(WG_THREADS);
+                  if (N < V) expert_sum_grad_kernel<X, 1, 4><<<n, b, 0, s>>>(a, at);
+                  else if (k <= 2) expert_sum_grad_kernel<X, V, 2><<<n, b, 0, s>>>(a, at);
+                  else if (k <= 4) expert_sum_grad_kernel<X, V, 4><<<n, b, 0, s>>>(a, at);
+                  else expert_sum_grad_kernel<X, V, 8><<<n, b, 0, s>>>(a, at);
+                });
               }));
 }
 
