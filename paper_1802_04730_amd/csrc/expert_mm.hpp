@@ -122,10 +122,11 @@ __device__ __forceinline__ bool expert_tile(const int* off, int E, int R, int bm
   return false;
 }
 
-// The first row of expert e: the most of Off(0..e).  (A trip to memory beside that of the expert's own: dW of 32 rows of 8 experts, 4096 x 2048, 29.2
-// us where 28.2 without, of 8020 rows of 64, 2672 x 1824, 202 and 196, of 16384 rows of 32, 2048 x 4096, 353 and 352.  Asked for before the expert is known: no faster.)
-__device__ __forceinline__ int expert_first_row(const int* off, int e, int R) {
-  const int lane = threadIdx.x & 63, own = offset_within(off, e, R);
+// The first row of expert e, which has rows by its own offsets: the most of Off(0..e); own: Off(e).  (A trip to memory beside that of the expert's
+// own: dW of 32 rows of 8 experts, 4096 x 2048, 29.2 us where 28.3 without, of 8020 rows of 64, 2672 x 1824, 199 and 197, of 16384 rows of 32, 2048 x 4096, 350
+// and 347.  Asked for before the expert is known, or looked at after the loop: no faster.)
+__device__ __forceinline__ int expert_first_row(const int* off, int e, int R, int own) {
+  const int lane = threadIdx.x & 63;
   int most = 0;
   if (e < 64) {
     most = offset_within(off, min(lane, e), R);
@@ -668,7 +669,9 @@ __global__ __launch_bounds__(64 * WM * WN) void expert_weights_kernel(ExpertWeig
   if (e >= p.E || in >= per) return;
   const int block = in / (8 * p.nt), rest = in % (8 * p.nt), height = min(8, p.mt - 8 * block);
   const int m0 = (8 * block + rest % height) * BM, n0 = (rest / height) * BN;
-  int lo = __builtin_amdgcn_readfirstlane(expert_first_row(p.off, e, p.R)), hi = max(lo, offset_within(p.off, e + 1, p.R));
+  int lo = offset_within(p.off, e, p.R), hi = offset_within(p.off, e + 1, p.R);
+  if (lo < hi) lo = __builtin_amdgcn_readfirstlane(expert_first_row(p.off, e, p.R, lo));
+  hi = max(lo, hi);
   if (p.parts > 1) {
     constexpr int BK = OpA::BK;
     const int share = (hi - lo + p.parts * BK - 1) / (p.parts * BK) * BK;
