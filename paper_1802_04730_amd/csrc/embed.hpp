@@ -2,8 +2,8 @@
 //   O(t,j)    = s * LUT(Idx(t), j)
 //   dLUT(e,j) (+)= s * sum over the t with Idx(t) = e of dO(t,j)
 // Both only move bytes.  A group of lanes takes up to 16 bytes each of a row, as many elements as make 16 bytes of the wider of input and
-// output; rows of any width start at any multiple of an element.  16384 rows of 4096 bfloat16: 44-47 us (5.7-6.1 TB/s, words that come again from
-// cache); 8 rows 2.8.
+// output; rows of any width start at any multiple of an element.  A call with 16384 rows of 4096 bfloat16 takes 43 us (6.3 TB/s: words that come again are read
+// from cache, 78 MB of 134 from memory), with 8 rows 3.3-3.7 (the kernel 2.5).
 //
 // The gradient walks the tokens sorted by number (key_sort.hpp) in chunks of EMBED_CHUNK places: a group of lanes adds up its chunk's rows of dO
 // in order, whose addresses are all known beforehand, and hands on a sum where the number changes.  Runs of one number
@@ -17,14 +17,16 @@
 
 namespace tc355 {
 
-// Places of a chunk.  Small ones spread few tokens over the device; long ones hand fewer partial sums on, which counts sooner where the table's rows of
-// zeros keep the device busy anyway.  us, 8 / 32 places, table written: 32000 x 2048 in fp32 of bfloat16, 4000 tokens 70 / 70, 9000: 90 / 85, 16000: 102 / 87;
-// 50000 x 4096 bfloat16 101 / 98, 124 / 109, 142 / 112; 5000 x 256 23 / 30, 38 / 42, 46 / 44.  Added to: 32 / 50, 53 / 65, 69 / 70, 20000: 76 / 74;
-// 37 / 57, 62 / 72, 89 / 79, 109 / 90; 24 / 33, 39 / 44, 46 / 46, 51 / 47.
+// Places of a chunk.  Small ones spread few tokens over the device; long ones hand fewer partial sums on, which counts sooner where a few numbers make up
+// much of the batch, as words do, and where a wide table's zeros keep the device busy anyway.  us, 8 / 32 places, numbers by Zipf's law (in brackets: all
+// equally often).  Table written, 8192, 14336 and 20000 tokens: 5000 x 256 bfloat16 37 / 40 (30 / 39), 45 / 44 (34 / 41), 50 / 45 (35 / 41); 32000 x 1024 46 / 44 (39 / 44), 58 / 51 (45 / 50),
+// 64 / 54 (48 / 52); 32000 x 2048 in fp32 of bfloat16 86 / 81 (78 / 80), 99 / 86 (90 / 89), 107 / 87 (90 / 88); the same of fp32 94 / 81 (83 / 82), 110 / 88 (99 / 91), 119 / 93 (104 / 96).
+// Added to: 5000 x 256 38 / 43 (31 / 42), 46 / 47 (34 / 44), 52 / 47 (36 / 43); 32000 x 2048 49 / 61 (50 / 65), 64 / 70 (70 / 76), 77 / 72 (87 / 89).
 constexpr int EMBED_CHUNK = 32;
 constexpr int EMBED_SMALL_CHUNK = 8;
-constexpr int EMBED_FEW_WRITTEN = 8192;  // so many tokens and more take long chunks where the table is written,
-constexpr int EMBED_FEW_ADDED = 14336;   // and where it is added to
+constexpr int EMBED_FEW = 14336;         // from so many tokens on chunks are long,
+constexpr int EMBED_FEW_WRITTEN = 8192;  // or from so many where a table of EMBED_WIDE columns or more is written
+constexpr int EMBED_WIDE = 512;
 
 struct EmbedArgs {
   const void* LUT;

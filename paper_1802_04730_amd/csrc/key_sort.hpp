@@ -5,7 +5,7 @@
 // No atomics on memory: the order, and with it every sum taken along it, is the same each time.
 //
 // Lanes of one digit find each other by a ballot per bit of the digit.  Bounded by the latency of a pass's launches at the sizes of a
-// training step (32768 keys of 18 bits: two passes of a count of 4.7 us and a placement of 9.7).  Up to SORT_SMALL keys are ranked by counting instead.
+// training step (32768 keys of 18 bits: two passes of a count of 4.7 us and a placement of 9.4).  Up to SORT_SMALL keys are ranked by counting instead.
 #pragma once
 #include "tc355_device.hpp"
 
@@ -183,7 +183,7 @@ static __global__ __launch_bounds__(SORT_THREADS) void sort_scatter_kernel(SortP
 
 // Few keys, n <= SORT_SMALL: every key's rank is counted among all of them, from LDS; a workgroup ranks 32, eight groups of 32 lanes
 // sharing the list.  n^2 comparisons, but one launch of one round trip to memory: 1500 keys in 5.8 us (all passes in one workgroup's LDS:
-// 8.5), and at 8192 the time of the passes (the whole gradient of 333 columns, 35.0 us at 8192, 35.4 at 8193).
+// 8.5), and at 8192 the time of the passes (the whole gradient of 333 columns, 31.9 us at 8192, 33.8 at 8193).
 static __global__ __launch_bounds__(WG_THREADS) void sort_rank_kernel(SortPass p) {
   constexpr int KEYS = 32, SHARES = WG_THREADS / KEYS;
   extern __shared__ __align__(16) int keys[];  // n, rounded up to a multiple of 32

@@ -84,8 +84,8 @@ EmbedGradPlan embed_grad_plan(int64_t E, int64_t D, int64_t T) {
   p.passes = (int)ceil_div(p.key_bits, SORT_MOST_BITS);
   p.bits = (int)ceil_div(p.key_bits, p.passes);
   p.tiles = ceil_div(T, SORT_TILE);
-  // (as many as a table that is added to has; never fewer than fewer tokens have: a workspace for more tokens serves fewer)
-  const int64_t chunks = std::max(ceil_div(T, EMBED_CHUNK), ceil_div(std::min<int64_t>(T, EMBED_FEW_ADDED), EMBED_SMALL_CHUNK));
+  // (as many as short chunks make; never fewer than fewer tokens have: a workspace for more tokens serves fewer)
+  const int64_t chunks = std::max(ceil_div(T, EMBED_CHUNK), ceil_div(std::min<int64_t>(T, EMBED_FEW), EMBED_SMALL_CHUNK));
   int64_t at = 0;
   const auto take = [&](int64_t n) {
     const int64_t o = at;
@@ -290,7 +290,7 @@ tc_status tc_embed_grad(const void* dO, const int32_t* Idx, void* dLUT, int64_t 
     EmbedGradArgs a{};
     a.dO = dO; a.dLUT = dLUT; a.part = T ? ws + pl.part : nullptr;
     a.T = (int)T; a.E = (int)E; a.D = (int)D; a.scale = scale; a.add = add != 0;
-    a.chunk = T < (add ? EMBED_FEW_ADDED : EMBED_FEW_WRITTEN) ? EMBED_SMALL_CHUNK : EMBED_CHUNK;
+    a.chunk = T < (add || D < EMBED_WIDE ? EMBED_FEW : EMBED_FEW_WRITTEN) ? EMBED_SMALL_CHUNK : EMBED_CHUNK;
     const int64_t chunks = ceil_div(T, a.chunk);
     a.lpr = 1;
     while (a.lpr < ceil_div(D, V) && a.lpr < WG_THREADS) a.lpr *= 2;
