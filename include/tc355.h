@@ -428,7 +428,8 @@ tc_status tc_lut(int32_t n_tables, const float *const *LUT,
  * Rows of a table of tokens, scaled:
  *     O(t,j) = scale * LUT(Idx(t), j)              t < T, j < D
  * LUT: [E,D]   Idx: [T] int32   O: [T,D], of LUT's type.
- * An index outside [0, E) reads nothing and gives a row of NaN, as in tc_lut.
+ * An index outside [0, E) reads nothing and gives a row of NaN, as in tc_lut, which
+ * in fp32 with scale 1 and one lookup is the same.
  */
 tc_status tc_embed(const void *LUT, const int32_t *Idx, void *O, int64_t E,
                    int64_t D, int64_t T, float scale, tc_type type,

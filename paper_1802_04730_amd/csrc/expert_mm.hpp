@@ -19,12 +19,12 @@
 //
 // Sums are fp32 in the matrix core's accumulators whatever the storage, and each output is rounded once.
 //
-// Measured, bfloat16: one matrix of 8192^3 785 us forward (1400 TFLOP/s, tile of 256), 1024 dX, 1081 dW (128); 32 experts of 512 rows each, N = 2048,
-// K = 4096: 282, 375, 382 us; of uneven shares 369-410, 360-413, 389-404: the last round of tiles, and last rows of experts, are
-// not full.  fp32, 2100 rows of 12 experts, 1001 x 517: 40, 50, 44 us.  Tried and left: two stages with all fragments read at once
+// Measured, us a call, bfloat16: one matrix of 8192^3 752 forward (1461 TFLOP/s, tile of 256), 961 dX, 1017 dW (128); 32 experts of 512 rows each, N = 2048,
+// K = 4096: 254, 323, 333; of uneven shares 344, 362, 387: the last round of tiles, and last rows of experts, are
+// not full.  fp32, 2100 rows of 12 experts, 1001 x 517: 38, 49, 42.  Tried and left: two stages with all fragments read at once
 // (uneven shares: 352, 538, 729 us, by spills), four stages of 64 bytes (404, 411, 539), 16 wavefronts a tile of 256 (spills), tiles of 256 x 128
 // in a ring of three (1088 TFLOP/s at 8192^3 where this then reached 1268, more lost at ragged ends), the last round's tiles shared by two
-// workgroups, and the next tile's first stages requested before this one is stored (no gain).
+// workgroups (no gain), and, for dW, the next tile's first stages requested before this one is stored (488 us from 486 at 32 experts, 2048 x 4096, 612 from 645 at 8, 4096 x 4096).
 #pragma once
 #include "expert_types.hpp"
 

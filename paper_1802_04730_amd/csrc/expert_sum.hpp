@@ -4,8 +4,8 @@
 //   dw(t,i)              = sum_n dO(t,n) * Y(Place(t,i), n)
 // Both only move bytes: every row of Y is read once, 16 bytes a lane, all k of a token in flight together.  A slot without a place (-1) takes
 // no part.  The gradient gives a token to one wavefront, which reads its row of dO once for all slots (for 8 of them at
-// a time) and sums dw over its lanes in a fixed order.  Measured at 8192 tokens, 4 rows of 2048 bfloat16: 30.6 us (5.5 TB/s) and
-// 54 us (5.6 TB/s); with a branch around each slot's load 60 and 52, with stores through the caches 42 and 52.
+// a time) and sums dw over its lanes in a fixed order.  Measured at 8192 tokens, 4 rows of 2048 bfloat16: 30 us (5.6 TB/s) and,
+// behind it, 54 us (5.6 TB/s; by itself, with nothing of Y in the caches, 71); with a branch around each slot's load 60 and 52, with stores through the caches 42 and 52.
 #pragma once
 #include <type_traits>
 

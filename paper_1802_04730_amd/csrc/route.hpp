@@ -13,8 +13,8 @@
 // rounds' latency, not the logits' bytes.  A workgroup takes ROUTE_TOKENS tokens and counts its slots per expert; the counts are
 // summed over the workgroups, and a last launch places the slots (key_sort.hpp's ranks by ballot).  Up to ROUTE_ALONE tokens
 // all of it is one workgroup's, in one launch.  No atomics on memory; integer ones in LDS.  Measured: 16 tokens of 64 experts, 4
-// chosen, 4.7 us; 16384 of 128, 8 chosen, 12.8 for the selection (29 by exchange through LDS), 4.2 for the sums, 6.3 for the places (63 where every
-// workgroup added the earlier ones' counts up), 9.6 for the gradient.
+// chosen, 4.8 us; 16384 of 128, 8 chosen, 12.5 for the selection (29 by exchange through LDS), 4.2 for the sums, 6.0 for the places (63 where every
+// workgroup added the earlier ones' counts up), 8.4-10.6 for the gradient.
 // The lines between the forms, us a call: one workgroup / two launches, 64 experts of which 4: 32 tokens 6.3 / 7.9, 48: 7.8 / 8.0, 64: 9.1 / 8.1; 128 of which 8:
 // 9.8 / 11.4, 14.2 / 11.6, 17.2 / 11.8; 256 of which 8: 37 / 39, 55 / 40, 71 / 40; 8 of which 2: 4.8 / 6.4, 5.5 / 6.5, 6.2 / 6.7.
 // Counts added up by every workgroup / by a launch of its own, 512, 1024 and 2048 tokens: 64 experts 9.4 / 11.4, 10.0 / 11.4, 12.2 / 11.7; 128: 13.4 / 15.0,
