@@ -1,5 +1,5 @@
 // Products grouped by expert where an expert has few rows (a decoding step): Y(r,n) = act(sum_k X(src(r),k) * W(e(r),n,k)).
-// What bounds it: the weights' bytes, each read for a handful of rows.  32 rows of 8 experts, 4096 x 2048 bfloat16: 27-29 us a call (4.6-4.9 TB/s of weights), the kernel 23.5 (5.7).
+// What bounds it: the weights' bytes, each read for a handful of rows.  32 rows of 8 experts, 4096 x 2048 bfloat16: 26-29 us a call (4.6-5.2 TB/s of weights), the kernel 23.5 (5.7).
 //
 // A workgroup computes 16 rows by 16 CT columns of one expert; its wavefronts share the reduction, in steps of 64 bytes of a row.
 // Operands go from memory to registers in the matrix instruction's layout -- nothing is used twice, so LDS would only be a
