@@ -62,6 +62,7 @@ template <int V>
 struct RowUnit {
   int c, skip;
   bool on;
+  RowUnit() = default;
   __device__ __forceinline__ RowUnit(int64_t u, int width) {
     const int64_t at = u * V;
     on = at < width;

@@ -30,6 +30,15 @@ typedef int (*expert_mm_grad_w_t)(const void*, const void*, const int32_t*, cons
                                   void*, size_t, void*);
 typedef int (*expert_sum_t)(const void*, const float*, const int32_t*, void*, int64_t, int64_t, int64_t, int64_t, int, void*);
 typedef int (*expert_sum_grad_t)(const void*, const void*, const float*, const int32_t*, void*, float*, int64_t, int64_t, int64_t, int64_t, int, void*);
+typedef int (*layer_norm_t)(const void*, const void*, const void*, void*, int64_t, int64_t, float, int, int, void*);
+typedef int (*layer_norm_grad_t)(const void*, const void*, const void*, void*, void*, void*, int64_t, int64_t, float, int32_t, int, int, void*, size_t, void*);
+typedef int (*route_balanced_t)(const void*, const float*, float*, int32_t*, int32_t*, int32_t*, int32_t*, int64_t, int64_t, int64_t, int64_t, int64_t, int32_t, int32_t,
+                                float, int, void*, size_t, void*);
+typedef int (*route_balanced_grad_t)(const void*, const int32_t*, const float*, void*, int64_t, int64_t, int64_t, int32_t, int32_t, float, int, void*);
+typedef int (*quantize_rows_t)(const void*, void*, void*, int64_t, int64_t, int, void*);
+typedef int (*quantize_weights_t)(const void*, void*, void*, void*, void*, int64_t, int64_t, int64_t, int, void*);
+typedef int (*expert_mm_q8_t)(const void*, const void*, const void*, const void*, const int32_t*, const int32_t*, const void*, void*, int64_t, int64_t, int64_t, int64_t,
+                              int64_t, int32_t, int, void*, size_t, void*);
 typedef int (*lut_t)(int32_t, const float* const*, const int32_t* const*, float* const*, const int64_t*, const int64_t*, int64_t, int64_t, void*);
 
 constexpr int kMost = 8;  // layers, tables
@@ -453,6 +462,142 @@ PyObject* call_expert_sum_grad(PyObject*, PyObject* const* v, Py_ssize_t n) {
   });
 }
 
+// ---- operators around experts of even load, with weights in 8 bits ----
+
+constexpr c10::ScalarType kQ8 = c10::ScalarType::Float8_e4m3fn, kScale = c10::ScalarType::Float8_e8m0fnu;
+constexpr int64_t kBlock = 128;
+int64_t blocks(int64_t n) { return (n + kBlock - 1) / kBlock; }
+bool is3(const Arg& a, int64_t x, int64_t y, int64_t z) { return a.size[0] == x && a.size[1] == y && a.size[2] == z; }
+bool vector_or_none(PyObject* o, const Kind& k, int64_t n, Arg* a) { return o == Py_None || (take(o, k.type, 1, a) && a->size[0] == n); }
+
+// (entry, X, W, B or None, O, eps, stream)
+PyObject* call_layer_norm(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  return guarded([&]() -> int {
+    Kind k, w;
+    Arg X, W, B, O;
+    void* s;
+    float eps;
+    if (n != 7 || !kind_of(v[1], &k) || !kind_of(v[2], &w) || (w.code != k.code && w.code != 0) || !take(v[1], k, 2, &X) || !take(v[2], w, 1, &W) ||
+        !take(v[4], k, 2, &O) || !number(v[5], &eps) || !stream_of(v[6], &s))
+      return -1;
+    const int64_t T = X.size[0], N = X.size[1];
+    layer_norm_t entry;
+    if (W.size[0] != N || !vector_or_none(v[3], w, N, &B) || !is(O, T, N) || !entry_of(v[0], &entry)) return -1;
+    return call(entry, (const void*)X.data, (const void*)W.data, (const void*)B.data, O.data, T, N, eps, k.code, w.code, s);
+  });
+}
+
+// (entry, dO, X, W, dX, dW or None, dB or None, workspace or None, eps, add, stream)
+PyObject* call_layer_norm_grad(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  return guarded([&]() -> int {
+    Kind k, w;
+    Arg d, X, W, G, gW, gB;
+    void *s, *ws;
+    size_t bytes;
+    float eps;
+    int32_t add;
+    if (n != 11 || !kind_of(v[1], &k) || !kind_of(v[3], &w) || (w.code != k.code && w.code != 0) || !take(v[1], k, 2, &d) || !take(v[2], k, 2, &X) ||
+        !take(v[3], w, 1, &W) || !take(v[4], k, 2, &G) || !workspace_of(v[7], &ws, &bytes) || !number(v[8], &eps) || !truth(v[9], &add) || !stream_of(v[10], &s))
+      return -1;
+    const int64_t T = X.size[0], N = X.size[1];
+    layer_norm_grad_t entry;
+    if (!is(d, T, N) || !is(G, T, N) || W.size[0] != N || !vector_or_none(v[5], w, N, &gW) || !vector_or_none(v[6], w, N, &gB) || !entry_of(v[0], &entry)) return -1;
+    return call(entry, (const void*)d.data, (const void*)X.data, (const void*)W.data, G.data, gW.data, gB.data, T, N, eps, add, k.code, w.code, ws, bytes, s);
+  });
+}
+
+// (entry, L, Bias or None, Wt, Id, Off, Row, Place, workspace or None, groups, keep, sigmoid, norm, scale, stream)
+PyObject* call_route_balanced(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  return guarded([&]() -> int {
+    Kind k;
+    Arg L, B, W, I, F, R, P;
+    void *s, *ws;
+    size_t bytes;
+    int64_t groups, keep;
+    int32_t sigmoid, norm;
+    float scale;
+    if (n != 15 || !kind_of(v[1], &k) || !take(v[1], k, 2, &L) || (v[2] != Py_None && !take(v[2], 1, &B)) || !take(v[3], 2, &W) || !take_ints(v[4], 2, &I) ||
+        !take_ints(v[5], 1, &F) || !take_ints(v[6], 1, &R) || !take_ints(v[7], 2, &P) || !workspace_of(v[8], &ws, &bytes) || !whole_number(v[9], &groups) ||
+        !whole_number(v[10], &keep) || !truth(v[11], &sigmoid) || !truth(v[12], &norm) || !number(v[13], &scale) || !stream_of(v[14], &s))
+      return -1;
+    const int64_t T = L.size[0], E = L.size[1], top = I.size[1];
+    route_balanced_t entry;
+    if (!is(I, T, top) || !is(W, T, top) || !is(P, T, top) || F.size[0] != E + 1 || R.size[0] != T * top || (B.size && B.size[0] != E) || !entry_of(v[0], &entry)) return -1;
+    return call(entry, (const void*)L.data, f(B), out(W), (int32_t*)I.data, (int32_t*)F.data, (int32_t*)R.data, (int32_t*)P.data, T, E, top, groups, keep, sigmoid, norm, scale,
+                k.code, ws, bytes, s);
+  });
+}
+
+// (entry, L, Id, dWt, dL, sigmoid, norm, scale, stream)
+PyObject* call_route_balanced_grad(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  return guarded([&]() -> int {
+    Kind k;
+    Arg L, I, W, G;
+    void* s;
+    int32_t sigmoid, norm;
+    float scale;
+    if (n != 9 || !kind_of(v[1], &k) || !take(v[1], k, 2, &L) || !take_ints(v[2], 2, &I) || !take(v[3], 2, &W) || !take(v[4], k, 2, &G) || !truth(v[5], &sigmoid) ||
+        !truth(v[6], &norm) || !number(v[7], &scale) || !stream_of(v[8], &s))
+      return -1;
+    const int64_t T = L.size[0], E = L.size[1], top = I.size[1];
+    route_balanced_grad_t entry;
+    if (!is(I, T, top) || !is(W, T, top) || !is(G, T, E) || !entry_of(v[0], &entry)) return -1;
+    return call(entry, (const void*)L.data, ints(I), f(W), G.data, T, E, top, sigmoid, norm, scale, k.code, s);
+  });
+}
+
+// (entry, X, Q, S, stream)
+PyObject* call_quantize_rows(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  return guarded([&]() -> int {
+    Kind k;
+    Arg X, Q, S;
+    void* s;
+    if (n != 5 || !kind_of(v[1], &k) || !take(v[1], k, 2, &X) || !take(v[2], kQ8, 2, &Q) || !take(v[3], kScale, 2, &S) || !stream_of(v[4], &s)) return -1;
+    const int64_t R = X.size[0], K = X.size[1], b = blocks(K);
+    quantize_rows_t entry;
+    if (!is(S, R, b) || !is(Q, R, kBlock * b) || !entry_of(v[0], &entry)) return -1;
+    return call(entry, (const void*)X.data, Q.data, S.data, R, K, k.code, s);
+  });
+}
+
+// (entry, W, Q, S, Qt or None, St or None, stream)
+PyObject* call_quantize_weights(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  return guarded([&]() -> int {
+    Kind k;
+    Arg W, Q, S, Qt, St;
+    void* s;
+    if (n != 7 || !kind_of(v[1], &k) || !take(v[1], k, 3, &W) || !take(v[2], kQ8, 3, &Q) || !take(v[3], kScale, 3, &S) || (v[4] != Py_None && !take(v[4], kQ8, 3, &Qt)) ||
+        (v[5] != Py_None && !take(v[5], kScale, 3, &St)) || !stream_of(v[6], &s))
+      return -1;
+    const int64_t E = W.size[0], N = W.size[1], K = W.size[2], nb = blocks(N), kb = blocks(K);
+    quantize_weights_t entry;
+    if (!is3(Q, E, N, kBlock * kb) || !is3(S, E, nb, kb) || (Qt.size && !is3(Qt, E, K, kBlock * nb)) || (St.size && !is3(St, E, kb, nb)) || !entry_of(v[0], &entry)) return -1;
+    return call(entry, (const void*)W.data, Q.data, S.data, Qt.data, St.data, E, N, K, k.code, s);
+  });
+}
+
+// (entry, X, SX or None, W, SW, Off or None, Row or None, gate or None, Y, workspace or None, relu, stream)
+PyObject* call_expert_mm_q8(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  return guarded([&]() -> int {
+    Kind k;
+    Arg X, SX, W, SW, F, Row, g, Y;
+    void *s, *ws;
+    size_t bytes;
+    int32_t relu;
+    if (n != 12 || !kind_of(v[8], &k) || !take(v[8], k, 2, &Y) || (v[2] == Py_None ? !take(v[1], k, 2, &X) : !take(v[1], kQ8, 2, &X) || !take(v[2], kScale, 2, &SX)) ||
+        !take(v[3], kQ8, 3, &W) || !take(v[4], kScale, 3, &SW) || !take_ints_or_none(v[5], 1, &F) || !take_ints_or_none(v[6], 1, &Row) || !take_or_none(v[7], k, 2, &g) ||
+        !workspace_of(v[9], &ws, &bytes) || !truth(v[10], &relu) || !stream_of(v[11], &s))
+      return -1;
+    const int64_t T = X.size[0], K = X.size[1], E = W.size[0], N = W.size[1], R = Y.size[0], kb = blocks(K);
+    expert_mm_q8_t entry;
+    if (W.size[2] != kBlock * kb || (SX.size && (K != kBlock * kb || !is(SX, T, kb))) || !is3(SW, E, blocks(N), kb) || Y.size[1] != N ||
+        (F.size ? F.size[0] != E + 1 : E != 1) || (Row.size ? Row.size[0] : T) != R || (g.size && !is(g, R, N)) || !entry_of(v[0], &entry))
+      return -1;
+    return call(entry, (const void*)X.data, (const void*)SX.data, (const void*)W.data, (const void*)SW.data, ints(F), ints(Row), (const void*)g.data, Y.data, T, R, E, N, K,
+                relu, k.code, ws, bytes, s);
+  });
+}
+
 template <PyObject* (*F)(PyObject*, PyObject* const*, Py_ssize_t)>
 PyMethodDef method(const char* name) {
   return {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(F)), METH_FASTCALL, nullptr};
@@ -464,6 +609,9 @@ PyMethodDef methods[] = {method<call_tbmm>("tbmm"),   method<call_tbmm_ws>("tbmm
                          method<call_route>("route"), method<call_route_grad>("route_grad"), method<call_expert_mm>("expert_mm"),
                          method<call_expert_mm_grad_x>("expert_mm_grad_x"), method<call_expert_mm_grad_w>("expert_mm_grad_w"),
                          method<call_expert_sum>("expert_sum"), method<call_expert_sum_grad>("expert_sum_grad"),
+                         method<call_layer_norm>("layer_norm"), method<call_layer_norm_grad>("layer_norm_grad"), method<call_route_balanced>("route_balanced"),
+                         method<call_route_balanced_grad>("route_balanced_grad"), method<call_quantize_rows>("quantize_rows"),
+                         method<call_quantize_weights>("quantize_weights"), method<call_expert_mm_q8>("expert_mm_q8"),
                          {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fast", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -22,6 +22,7 @@
 #pragma once
 #include "expert_types.hpp"
 #include "key_sort.hpp"
+#include "lanes.hpp"
 
 namespace tc355 {
 
@@ -50,26 +51,6 @@ __device__ __forceinline__ unsigned route_order(float x) {  // orders as the log
   const unsigned o = b & 0x80000000u ? ~b : b | 0x80000000u;
   return o - 0x007fffffu;  // (-inf is the lowest: 0x007fffff)
 }
-
-// f(x, y) over the G lanes of a group, in all of them: y of another lane.  Rows of 16 lanes by moves between lanes, beyond by LDS.
-template <int CTRL, typename X>
-__device__ __forceinline__ X from_lane(X x) {
-  return __builtin_bit_cast(X, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xf, 0xf, true));
-}
-template <int G, typename X, typename F>
-__device__ __forceinline__ X group_all(X x, F f) {
-  x = f(x, from_lane<0xB1>(x));   // lane ^ 1
-  x = f(x, from_lane<0x4E>(x));   // lane ^ 2
-  x = f(x, from_lane<0x141>(x));  // 7 - lane of 8: the other four
-  x = f(x, from_lane<0x140>(x));  // 15 - lane: the other eight
-#pragma unroll
-  for (int d = 16; d < G; d *= 2) x = f(x, __shfl_xor(x, d));
-  return x;
-}
-__device__ __forceinline__ float most_of(float a, float b) { return fmaxf(a, b); }
-__device__ __forceinline__ float sum_of(float a, float b) { return a + b; }
-__device__ __forceinline__ unsigned larger(unsigned a, unsigned b) { return a > b ? a : b; }
-__device__ __forceinline__ int smaller(int a, int b) { return a < b ? a : b; }
 
 // A lane's logits: V neighbours from column c on, in as few loads as they fit; -inf past the end.
 template <typename T, int V>
@@ -123,6 +104,30 @@ __device__ __forceinline__ void route_place(const RouteArgs& p, int tile, const 
       p.Row[r] = e < 0 ? -1 : (int)(s / p.k);
     }
   }
+}
+
+// What follows the selection: mem holds the workgroup's slots of each expert.  They go to memory, or, where one workgroup does it all, turn into starts,
+// and the slots are placed.
+__device__ __forceinline__ void route_counted(const RouteArgs& p, int* mem, int* part) {
+  const int bins = 1 << p.bits;
+  __syncthreads();
+  if (p.count) {
+    for (int b = threadIdx.x; b < bins; b += WG_THREADS) p.count[(int64_t)b * (p.tiles + 1) + blockIdx.x] = mem[b];
+    return;
+  }
+  // one workgroup: counts to starts, then the places
+  __threadfence_block();
+  int run = 0;
+  for (int b0 = 0; b0 < bins; b0 += WG_THREADS) {
+    const int b = b0 + threadIdx.x, c = b < bins ? mem[b] : 0;
+    int total;
+    const int lower = block_prefix<WAVES_PER_WG>(c, part, &total);
+    if (b < bins) mem[b] = run + lower;
+    run += total;
+    if (b <= p.E) p.Off[b] = mem[b];
+  }
+  __syncthreads();
+  route_place(p, 0, mem, mem + bins);
 }
 
 template <typename T, int G, int V>
@@ -191,24 +196,7 @@ __global__ __launch_bounds__(WG_THREADS) void route_kernel(RouteArgs p) {
       }
     }
   }
-  __syncthreads();
-  if (p.count) {
-    for (int b = threadIdx.x; b < bins; b += WG_THREADS) p.count[(int64_t)b * (p.tiles + 1) + blockIdx.x] = mem[b];
-    return;
-  }
-  // one workgroup: counts to starts, then the places
-  __threadfence_block();
-  int run = 0;
-  for (int b0 = 0; b0 < bins; b0 += WG_THREADS) {
-    const int b = b0 + threadIdx.x, c = b < bins ? mem[b] : 0;
-    int total;
-    const int lower = block_prefix<WAVES_PER_WG>(c, part, &total);
-    if (b < bins) mem[b] = run + lower;
-    run += total;
-    if (b <= p.E) p.Off[b] = mem[b];
-  }
-  __syncthreads();
-  route_place(p, 0, mem, mem + bins);
+  route_counted(p, mem, part);
 }
 
 static __global__ __launch_bounds__(WG_THREADS) void route_place_kernel(RouteArgs p) {

@@ -36,13 +36,16 @@ TC_MLP_AUTO, TC_MLP_ROWS, TC_MLP_TILES, TC_MLP_PER_LAYER = 0, 1, 2, 3
 # storage types of the operators around experts (tc_type)
 TC_F32, TC_BF16, TC_F16 = 0, 1, 2
 _TYPES = {torch.float32: TC_F32, torch.bfloat16: TC_BF16, torch.float16: TC_F16}
+TC_Q8_BLOCK = 128  # elements of a scale of 8-bit operands
 
 EXPORTS = ["tc_status_string", "tc355_version", "tc355_set_option", "tc355_get_option", "tc355_last_path", "tc_tbmm", "tc_tbmm_ws", "tc_tbmm_workspace_bytes", "tc_mlp_fcrelu", "tc_mlp_fcrelu_workspace_bytes",
            "tc_mlp_fcrelu_static",
            "tc_group_conv", "tc_group_conv_infer", "tc_kron", "tc_sconv2d", "tc_sconv2d_infer", "tc_lut",
            "tc_embed", "tc_embed_grad", "tc_embed_grad_workspace_bytes", "tc_route", "tc_route_workspace_bytes", "tc_route_grad",
            "tc_expert_mm", "tc_expert_mm_grad_x", "tc_expert_mm_grad_w", "tc_expert_mm_grad_w_workspace_bytes", "tc_expert_sum",
-           "tc_expert_sum_grad"]
+           "tc_expert_sum_grad",
+           "tc_layer_norm", "tc_layer_norm_grad", "tc_layer_norm_grad_workspace_bytes", "tc_route_balanced", "tc_route_balanced_workspace_bytes",
+           "tc_route_balanced_grad", "tc_quantize_rows", "tc_quantize_weights", "tc_expert_mm_q8", "tc_expert_mm_q8_workspace_bytes"]
 
 
 _RAW_STREAM = getattr(torch._C, "_cuda_getCurrentRawStream", None)
@@ -105,10 +108,18 @@ def lib() -> ctypes.CDLL:
                        "tc_expert_mm_grad_x": [vp] * 5 + [i64] * 4 + [kind, vp],
                        "tc_expert_mm_grad_w": [vp] * 5 + [i64] * 5 + [i32, kind, kind, vp, size, vp],
                        "tc_expert_sum": [vp] * 4 + [i64] * 4 + [kind, vp],
-                       "tc_expert_sum_grad": [vp] * 6 + [i64] * 4 + [kind, vp]}.items():
+                       "tc_expert_sum_grad": [vp] * 6 + [i64] * 4 + [kind, vp],
+                       "tc_layer_norm": [vp] * 4 + [i64, i64, f32, kind, kind, vp],
+                       "tc_layer_norm_grad": [vp] * 6 + [i64, i64, f32, i32, kind, kind, vp, size, vp],
+                       "tc_route_balanced": [vp] * 7 + [i64] * 5 + [i32, i32, f32, kind, vp, size, vp],
+                       "tc_route_balanced_grad": [vp] * 4 + [i64, i64, i64, i32, i32, f32, kind, vp],
+                       "tc_quantize_rows": [vp] * 3 + [i64, i64, kind, vp],
+                       "tc_quantize_weights": [vp] * 5 + [i64, i64, i64, kind, vp],
+                       "tc_expert_mm_q8": [vp] * 8 + [i64] * 5 + [i32, kind, vp, size, vp]}.items():
         getattr(L, name).argtypes = args
         getattr(L, name).restype = ctypes.c_int
-    for name, n in (("tc_embed_grad_workspace_bytes", 3), ("tc_route_workspace_bytes", 3), ("tc_expert_mm_grad_w_workspace_bytes", 4)):
+    for name, n in (("tc_embed_grad_workspace_bytes", 3), ("tc_route_workspace_bytes", 3), ("tc_expert_mm_grad_w_workspace_bytes", 4),
+                    ("tc_layer_norm_grad_workspace_bytes", 2), ("tc_route_balanced_workspace_bytes", 3), ("tc_expert_mm_q8_workspace_bytes", 5)):
         getattr(L, name).argtypes = [i64] * n
         getattr(L, name).restype = size
     _load_fast(L)
@@ -133,7 +144,8 @@ def _load_fast(L) -> None:
                       RuntimeWarning, stacklevel=3)
         return
     for name in ("tc_tbmm", "tc_tbmm_ws", "tc_mlp_fcrelu", "tc_group_conv", "tc_kron", "tc_sconv2d", "tc_lut", "tc_embed", "tc_embed_grad", "tc_route",
-                 "tc_route_grad", "tc_expert_mm", "tc_expert_mm_grad_x", "tc_expert_mm_grad_w", "tc_expert_sum", "tc_expert_sum_grad"):
+                 "tc_route_grad", "tc_expert_mm", "tc_expert_mm_grad_x", "tc_expert_mm_grad_w", "tc_expert_sum", "tc_expert_sum_grad",
+                 "tc_layer_norm", "tc_layer_norm_grad", "tc_route_balanced", "tc_route_balanced_grad", "tc_quantize_rows", "tc_quantize_weights", "tc_expert_mm_q8"):
         _AT[name] = ctypes.cast(getattr(L, name), ctypes.c_void_p).value
     _FAST = fast
 
@@ -554,3 +566,136 @@ def tc_expert_sum_grad(dO, Y, Wt, Place, dY, dWt, stream=None) -> None:
     (R, N), (T, k) = Y.shape, Place.shape
     _fit(tuple(dO.shape) == (T, N) and tuple(Wt.shape) == tuple(dWt.shape) == (T, k) and dY.shape == Y.shape, "tc_expert_sum_grad")
     _check(lib().tc_expert_sum_grad(*args, T, R, k, N, _TYPES[dO.dtype], _stream(stream)), "tc_expert_sum_grad")
+
+
+# ---- operators around experts of even load, with weights in 8 bits ------------------------------------------------------------------
+
+
+def tc_layer_norm(X, W, B, O, eps: float = 1e-5, stream=None) -> None:
+    """O[T,N] = (X[T,N] - mean) / sqrt(variance + eps) * W[N] + B[N] (None: zeros), row by row; W and B of X's type or float32."""
+    if _FAST is not None:
+        status = _FAST.layer_norm(_AT["tc_layer_norm"], X, W, B, O, eps, stream)
+        if status >= 0:
+            return _check(status, "tc_layer_norm")
+    x, o = _typed(X, "X", 2), _typed(O, "O", 2, X.dtype)
+    w = _grad_of(W, "W", 1, X.dtype)
+    b = None if B is None else _typed(B, "B", 1, W.dtype)
+    T, N = X.shape
+    _fit(O.shape == X.shape and W.shape[0] == N and (B is None or B.shape[0] == N), "tc_layer_norm")
+    _check(lib().tc_layer_norm(x, w, b, o, T, N, eps, _TYPES[X.dtype], _TYPES[W.dtype], _stream(stream)), "tc_layer_norm")
+
+
+def tc_layer_norm_grad_workspace_bytes(T: int, N: int) -> int:
+    return int(lib().tc_layer_norm_grad_workspace_bytes(int(T), int(N)))
+
+
+def tc_layer_norm_grad(dO, X, W, dX, dW, dB, workspace=None, eps: float = 1e-5, add: bool = False, stream=None) -> None:
+    """dX[T,N] and, (+)=, dW[N] and dB[N] (None: not asked for; dB only beside dW): the gradients of tc_layer_norm, from dO[T,N].
+
+    ``workspace``: a uint8 tensor of at least tc_layer_norm_grad_workspace_bytes(T, N) bytes (None without dW)."""
+    if _FAST is not None:
+        status = _FAST.layer_norm_grad(_AT["tc_layer_norm_grad"], dO, X, W, dX, dW, dB, workspace, eps, add, stream)
+        if status >= 0:
+            return _check(status, "tc_layer_norm_grad")
+    x, d, g = _typed(X, "X", 2), _typed(dO, "dO", 2, X.dtype), _typed(dX, "dX", 2, X.dtype)
+    w = _grad_of(W, "W", 1, X.dtype)
+    gw, gb = (None if t is None else _typed(t, n, 1, W.dtype) for t, n in ((dW, "dW"), (dB, "dB")))
+    T, N = X.shape
+    _fit(dO.shape == dX.shape == X.shape and W.shape[0] == N and all(t is None or t.shape[0] == N for t in (dW, dB)), "tc_layer_norm_grad")
+    wp, wn = _workspace(workspace)
+    _check(lib().tc_layer_norm_grad(d, x, w, g, gw, gb, T, N, eps, int(add), _TYPES[X.dtype], _TYPES[W.dtype], wp, wn, _stream(stream)), "tc_layer_norm_grad")
+
+
+def tc_route_balanced_workspace_bytes(T: int, E: int, k: int) -> int:
+    return int(lib().tc_route_balanced_workspace_bytes(int(T), int(E), int(k)))
+
+
+def tc_route_balanced(L, Bias, Wt, Id, Off, Row, Place, workspace=None, groups: int = 1, keep: int = 1, sigmoid: bool = False, norm: bool = False,
+                      scale: float = 1.0, stream=None) -> None:
+    """tc_route by scores of sigmoid or softmax: the k largest of score + Bias[E] (None: zeros) in the `keep` best of `groups` groups, weights of
+    scale times the scores (norm: over their sum).
+
+    ``workspace``: a uint8 tensor of at least tc_route_balanced_workspace_bytes(T, E, k) bytes, as for tc_route."""
+    if _FAST is not None:
+        status = _FAST.route_balanced(_AT["tc_route_balanced"], L, Bias, Wt, Id, Off, Row, Place, workspace, groups, keep, sigmoid, norm, scale, stream)
+        if status >= 0:
+            return _check(status, "tc_route_balanced")
+    i32 = torch.int32
+    args = (_typed(L, "L", 2), None if Bias is None else _typed(Bias, "Bias", 1, torch.float32), _typed(Wt, "Wt", 2, torch.float32), _typed(Id, "Id", 2, i32),
+            _typed(Off, "Off", 1, i32), _typed(Row, "Row", 1, i32), _typed(Place, "Place", 2, i32))
+    (T, E), k = L.shape, Id.shape[1]
+    _fit(tuple(Id.shape) == tuple(Wt.shape) == tuple(Place.shape) == (T, k) and Off.shape[0] == E + 1 and Row.shape[0] == T * k and
+         (Bias is None or Bias.shape[0] == E), "tc_route_balanced")
+    wp, wn = _workspace(workspace)
+    _check(lib().tc_route_balanced(*args, T, E, k, groups, keep, int(sigmoid), int(norm), scale, _TYPES[L.dtype], wp, wn, _stream(stream)), "tc_route_balanced")
+
+
+def tc_route_balanced_grad(L, Id, dWt, dL, sigmoid: bool = False, norm: bool = False, scale: float = 1.0, stream=None) -> None:
+    """dL[T,E]: the gradient of tc_route_balanced's weights, from L[T,E], Id[T,k] and dWt[T,k]."""
+    if _FAST is not None:
+        status = _FAST.route_balanced_grad(_AT["tc_route_balanced_grad"], L, Id, dWt, dL, sigmoid, norm, scale, stream)
+        if status >= 0:
+            return _check(status, "tc_route_balanced_grad")
+    args = (_typed(L, "L", 2), _typed(Id, "Id", 2, torch.int32), _typed(dWt, "dWt", 2, torch.float32), _typed(dL, "dL", 2, L.dtype))
+    (T, E), k = L.shape, Id.shape[1]
+    _fit(tuple(Id.shape) == tuple(dWt.shape) == (T, k) and dL.shape == L.shape, "tc_route_balanced_grad")
+    _check(lib().tc_route_balanced_grad(*args, T, E, k, int(sigmoid), int(norm), scale, _TYPES[L.dtype], _stream(stream)), "tc_route_balanced_grad")
+
+
+def _blocks(n: int) -> int:
+    return -(-n // TC_Q8_BLOCK)
+
+
+def tc_quantize_rows(X, Q, S, stream=None) -> None:
+    """Q[R,K'] (float8_e4m3fn) and S[R,K'/128] (float8_e8m0fnu): the rows of X[R,K] in 8 bits, a scale for each 128 elements; K': K rounded up to 128s."""
+    if _FAST is not None:
+        status = _FAST.quantize_rows(_AT["tc_quantize_rows"], X, Q, S, stream)
+        if status >= 0:
+            return _check(status, "tc_quantize_rows")
+    args = (_typed(X, "X", 2), _typed(Q, "Q", 2, torch.float8_e4m3fn), _typed(S, "S", 2, torch.float8_e8m0fnu))
+    R, K = X.shape
+    _fit(tuple(S.shape) == (R, _blocks(K)) and tuple(Q.shape) == (R, TC_Q8_BLOCK * _blocks(K)), "tc_quantize_rows")
+    _check(lib().tc_quantize_rows(*args, R, K, _TYPES[X.dtype], _stream(stream)), "tc_quantize_rows")
+
+
+def tc_quantize_weights(W, Q, S, Qt=None, St=None, stream=None) -> None:
+    """Q[E,N,K'], S[E,N'/128,K'/128]: the weights W[E,N,K] in 8 bits, a scale for each 128 x 128 elements; Qt[E,K,N'], St[E,K'/128,N'/128] (both or
+    neither): the same transposed."""
+    if _FAST is not None:
+        status = _FAST.quantize_weights(_AT["tc_quantize_weights"], W, Q, S, Qt, St, stream)
+        if status >= 0:
+            return _check(status, "tc_quantize_weights")
+    e4, e8 = torch.float8_e4m3fn, torch.float8_e8m0fnu
+    args = (_typed(W, "W", 3), _typed(Q, "Q", 3, e4), _typed(S, "S", 3, e8), None if Qt is None else _typed(Qt, "Qt", 3, e4), None if St is None else _typed(St, "St", 3, e8))
+    E, N, K = W.shape
+    n, k = _blocks(N), _blocks(K)
+    _fit(tuple(Q.shape) == (E, N, TC_Q8_BLOCK * k) and tuple(S.shape) == (E, n, k) and (Qt is None or tuple(Qt.shape) == (E, K, TC_Q8_BLOCK * n)) and
+         (St is None or tuple(St.shape) == (E, k, n)), "tc_quantize_weights")
+    _check(lib().tc_quantize_weights(*args, E, N, K, _TYPES[W.dtype], _stream(stream)), "tc_quantize_weights")
+
+
+def tc_expert_mm_q8_workspace_bytes(T: int, R: int, E: int, N: int, K: int) -> int:
+    return int(lib().tc_expert_mm_q8_workspace_bytes(int(T), int(R), int(E), int(N), int(K)))
+
+
+def tc_expert_mm_q8(X, SX, W, SW, Off, Row, gate, Y, workspace=None, relu: bool = False, stream=None) -> None:
+    """tc_expert_mm with weights W[E,N,K'], SW[E,N'/128,K'/128] in 8 bits (tc_quantize_weights) and rows X[T,K] put in 8 bits on the way, or X[T,K'], SX[T,K'/128]
+    that are already; 0 where gate[R,N] (or None) is not above 0.  Off None: one expert (E = 1) has all rows.
+
+    With dY for X and the transposed weights for W: the gradient of the rows.  ``workspace``: a uint8 tensor of at least
+    tc_expert_mm_q8_workspace_bytes(T, R, E, N, K) bytes (None where X is in 8 bits)."""
+    if _FAST is not None:
+        status = _FAST.expert_mm_q8(_AT["tc_expert_mm_q8"], X, SX, W, SW, Off, Row, gate, Y, workspace, relu, stream)
+        if status >= 0:
+            return _check(status, "tc_expert_mm_q8")
+    i32, e4, e8 = torch.int32, torch.float8_e4m3fn, torch.float8_e8m0fnu
+    y = _typed(Y, "Y", 2)
+    args = (_typed(X, "X", 2, Y.dtype if SX is None else e4), None if SX is None else _typed(SX, "SX", 2, e8), _typed(W, "W", 3, e4), _typed(SW, "SW", 3, e8),
+            None if Off is None else _typed(Off, "Off", 1, i32), None if Row is None else _typed(Row, "Row", 1, i32),
+            None if gate is None else _typed(gate, "gate", 2, Y.dtype), y)
+    (T, K), (E, N, K8), R = X.shape, W.shape, Y.shape[0]
+    k = _blocks(K)
+    _fit(K8 == TC_Q8_BLOCK * k and (SX is None or (K == K8 and tuple(SX.shape) == (T, k))) and tuple(SW.shape) == (E, _blocks(N), k) and Y.shape[1] == N and
+         (E == 1 if Off is None else Off.shape[0] == E + 1) and (T if Row is None else Row.shape[0]) == R and (gate is None or gate.shape == Y.shape), "tc_expert_mm_q8")
+    wp, wn = _workspace(workspace)
+    _check(lib().tc_expert_mm_q8(*args, T, R, E, N, K, int(relu), _TYPES[Y.dtype], wp, wn, _stream(stream)), "tc_expert_mm_q8")
