@@ -16,6 +16,8 @@
 #include "expert_mm.hpp"
 #include "quantize8.hpp"
 
+#include <type_traits>
+
 namespace tc355 {
 
 typedef int i8v __attribute__((ext_vector_type(8)));
@@ -56,11 +58,11 @@ __device__ __forceinline__ unsigned q8_scales(const unsigned char* row, int s, i
   return v;
 }
 
-// acc += the products of a stage: w and x 32 bytes of a row each, sw and sx their scales' lowest bytes.
-template <typename T>
+// acc += the products of a stage: w and x 32 bytes of a row each, their scales bytes SW of sw and SX of sx.
+template <typename T, int SW, int SX>
 __device__ __forceinline__ f4 q8_mfma(const i8v& w, const i8v& x, f4 acc, unsigned sw, unsigned sx) {
   if constexpr (sizeof(T) == 2) {
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x, acc, 0, 0, 0, (int)sw, 0, (int)sx);
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x, acc, 0, 0, SW, (int)sw, SX, (int)sx);
   } else {
     f4 sum = {0, 0, 0, 0};
     typedef Elem<f16>::v8 v8;
@@ -76,7 +78,7 @@ __device__ __forceinline__ f4 q8_mfma(const i8v& w, const i8v& x, f4 acc, unsign
       }
       sum = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, sum, 0, 0, 0);
     }
-    const int a = (int)(sw & 255), b = (int)(sx & 255);
+    const int a = (int)(sw >> (8 * SW) & 255), b = (int)(sx >> (8 * SX) & 255);
     const bool nan = a == (int)Q8_NAN || b == (int)Q8_NAN;
 #pragma unroll
     for (int v = 0; v < 4; v++) acc[v] += nan ? __builtin_nanf("") : __builtin_amdgcn_ldexpf(sum[v], a + b - 254);
@@ -84,59 +86,42 @@ __device__ __forceinline__ f4 q8_mfma(const i8v& w, const i8v& x, f4 acc, unsign
   }
 }
 
-// The fragments of M blocks of 16 rows from row r0 on.
-template <int M>
-__device__ __forceinline__ void q8_fragments(const lds_char* lds, int r0, int i, int q, i8v (&f)[M]) {
-#pragma unroll
-  for (int m = 0; m < M; m++) {
-    const char __attribute__((address_space(3)))* row = lds + (r0 + 16 * m + i) * EMM_STAGE;
-    const u4 lo = *(const __attribute__((address_space(3))) u4*)(row + ((q ^ (i & 7)) * 16)), hi = *(const __attribute__((address_space(3))) u4*)(row + (((4 + q) ^ (i & 7)) * 16));
-    f[m] = i8v{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+template <int I>
+using Q8Int = std::integral_constant<int, I>;
+// f(integral constants 0 .. N-1), in turn.
+template <int N, int I = 0, typename F>
+__device__ __forceinline__ void q8_for(F f) {
+  if constexpr (I < N) {
+    f(Q8Int<I>{});
+    q8_for<N, I + 1>(f);
   }
 }
 
-// ROWS rows of 128 bytes a stage to LDS, 8 rows an instruction, NW wavefronts; rows lie anywhere.
-template <int ROWS, int NW>
-struct Q8Rows {
-  static constexpr int BYTES = ROWS * EMM_STAGE, PER = ROWS / 8 / NW;
-  static_assert(PER * 8 * NW == ROWS, "whole instructions");
-  const char* p[PER];
-  template <typename F>
-  __device__ __forceinline__ void begin(const unsigned char* b, int64_t ld, int wave, int lane, F row) {
-#pragma unroll
-    for (int j = 0; j < PER; j++) p[j] = reinterpret_cast<const char*>(b) + row((wave * PER + j) * 8 + (lane >> 3)) * ld + ((lane & 7) ^ (lane >> 3)) * 16;
-  }
-  __device__ __forceinline__ void to_lds(lds_char* lds, int wave) {
-#pragma unroll
-    for (int j = 0; j < PER; j++) {
-      emm_to_lds(p[j], lds + (wave * PER + j) * 1024);
-      p[j] += EMM_STAGE;
-    }
-  }
-};
-
-// Reads of the next fragments and loads of a later stage.  (Restricted pointers of a function of their own, as emm_traffic's.)
-template <int MH, int NI, typename A, typename B>
-__device__ __forceinline__ void q8_traffic(A& a, B& b, const lds_char* __restrict__ now, lds_char* __restrict__ then, bool rows, bool cols, bool more, int rm, int cn, int wave,
-                                           int lane, i8v (&fa)[MH], i8v (&fb)[NI]) {
-  if (more) {
-    a.to_lds(then, wave);
-    b.to_lds(then + A::BYTES, wave);
-  }
-  if (cols) q8_fragments<NI>(now + A::BYTES, cn, lane & 15, lane >> 4, fb);
-  if (rows) q8_fragments<MH>(now, rm, lane & 15, lane >> 4, fa);
+// 16 bytes a lane straight to LDS, lane l's to `lds` + 16 l (both uniform).  In asm, so that the compiler does not take every later LDS read for one of these bytes and
+// wait for them: who reads them waits by emm_wait<0> and a barrier.
+__device__ __forceinline__ void q8_to_lds(const char* p, unsigned lds) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(p), "s"(lds) : "memory", "m0");
+}
+__device__ __forceinline__ void q8_to_lds(const char* base, unsigned off, unsigned lds) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(lds) : "memory", "m0");
 }
 
+constexpr int Q8_CHUNK = 64;  // stages whose scales are in LDS
+
+// Each wavefront multiplies MI x NI blocks of 16 x 16, a stage in MI steps.  A step multiplies one block of 16 rows with all columns while the next block's fragment is
+// read.  Before the last step a barrier: the next stage is in LDS, and nobody reads this one any more; so the last step replaces each column's fragment by the next stage's, as soon as it
+// is used, and requests the stage after that.  Four wavefronts: 128 x 128 of a tile of 256 each read a third less from LDS (128 KB a stage) than eight, whose
+// reads and the loads' writes would take as long as the products; a wavefront has all 512 registers of its SIMD's lanes, half of them sums.
 template <typename T, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(64 * WM * WN) void expert_mm_q8_kernel(Q8Args p) {
-  constexpr int NW = WM * WN, MI = BM / WM / 16, NI = BN / WN / 16, MH = MI / 2;
-  static_assert(MH * 2 == MI, "two halves");
-  typedef Q8Rows<BM, NW> OpA;
-  typedef Q8Rows<BN, NW> OpB;
-  constexpr int STAGE = OpA::BYTES + OpB::BYTES, LOADS = OpA::PER + OpB::PER;
-  constexpr int OUT = BM * BN * sizeof(T);
-  __shared__ __align__(16) char lds[2 * STAGE > OUT ? 2 * STAGE : OUT];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15;
+  constexpr int NW = WM * WN, MI = BM / WM / 16, NI = BN / WN / 16;
+  constexpr int PA = BM / 8 / NW, PB = BN / 8 / NW;  // loads of a wavefront a stage, 8 rows each
+  constexpr int BLOCKS = (BN + Q8_BLOCK - 1) / Q8_BLOCK;
+  static_assert(MI % 2 == 0 && PA * 8 * NW == BM && PB * 8 * NW == BN && BN / WN <= Q8_BLOCK, "whole steps, loads and blocks");
+  constexpr int BYTES_A = BM * EMM_STAGE, STAGE = (BM + BN) * EMM_STAGE;
+  constexpr int SCALES = Q8_CHUNK * (BM + BLOCKS), OUT = BM * BN * sizeof(T);
+  __shared__ __align__(16) char lds[2 * STAGE + SCALES > OUT ? 2 * STAGE + SCALES : OUT];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, q = lane >> 4;
   ExpertTile t;
   if (!q8_tile(p, BM, &t)) return;
   const int lo = __builtin_amdgcn_readfirstlane(t.lo), hi = __builtin_amdgcn_readfirstlane(t.hi), e = __builtin_amdgcn_readfirstlane(t.e);
@@ -154,86 +139,149 @@ __global__ __launch_bounds__(64 * WM * WN) void expert_mm_q8_kernel(Q8Args p) {
       const int r = min(m0 + j, hi - 1);  // (rows past the expert's: any will do)
       return p.row ? min(max(p.row[r], 0), p.T - 1) : r;
     };
-    OpA a;
-    OpB b;
-    a.begin(p.A, ld, wave, lane, source);
-    const int most = p.NO - 1 - n0;
-    b.begin(p.W + ((int64_t)e * p.NO + n0) * ld, ld, wave, lane, [&](int j) -> int64_t { return min(j, most); });
-    // scales: four stages' in a word, of this lane's rows and of the wavefront's columns (which share a block)
-    const unsigned char* sa[MI];
+    const int most = p.NO - 1 - n0, nb = (p.NO + Q8_BLOCK - 1) / Q8_BLOCK;
+    const lds_char* const mem = (lds_char*)lds;
+    const unsigned base = (unsigned)(uintptr_t)mem;
+    lds_char* const scales = (lds_char*)lds + 2 * STAGE;
+    // this lane's rows of the loads, at its chunk of the stage
+    const char* a[PA];
+    unsigned b[PB];
+    const char* w = reinterpret_cast<const char*>(p.W) + ((int64_t)e * p.NO + n0) * ld;
+    const int chunk = ((lane & 7) ^ (lane >> 3)) * 16;
 #pragma unroll
-    for (int m = 0; m < MI; m++) sa[m] = p.SA + source(rm + 16 * m + i) * p.stages;
-    const int nb = (p.NO + Q8_BLOCK - 1) / Q8_BLOCK;
-    const unsigned char* const sw = p.SW + ((int64_t)e * nb + min((n0 + cn) / Q8_BLOCK, nb - 1)) * p.stages;
-    unsigned va[MI], vw, na[MI], nw;
+    for (int j = 0; j < PA; j++) a[j] = reinterpret_cast<const char*>(p.A) + source((wave * PA + j) * 8 + (lane >> 3)) * ld + chunk;
 #pragma unroll
-    for (int m = 0; m < MI; m++) na[m] = q8_scales(sa[m], 0, p.stages);
-    nw = q8_scales(sw, 0, p.stages);
-    i8v fa[2][MH], fb[2][NI];
-    lds_char* const mem = (lds_char*)lds;
-    a.to_lds(mem, wave);
-    b.to_lds(mem + OpA::BYTES, wave);
-    if (p.stages > 1) {
-      a.to_lds(mem + STAGE, wave);
-      b.to_lds(mem + STAGE + OpA::BYTES, wave);
-      emm_wait<LOADS>();
-    } else {
-      emm_wait<0>();
-    }
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-    q8_traffic<MH, NI>(a, b, mem, mem, true, true, false, rm, cn, wave, lane, fa[0], fb[0]);
-    const auto stage = [&](int s, lds_char* now, lds_char* next, i8v (&f)[NI], i8v (&g)[NI]) {
-      if ((s & 3) == 0) {
+    for (int j = 0; j < PB; j++) b[j] = (unsigned)(min((wave * PB + j) * 8 + (lane >> 3), most) * ld) + chunk;
+    const auto load = [&](auto j, unsigned to) {  // one of the wavefront's loads
+      constexpr int J = decltype(j)::value;
+      if constexpr (J < PA) {
+        q8_to_lds(a[J], base + to + (wave * PA + J) * 1024);
+        a[J] += EMM_STAGE;
+      } else {
+        q8_to_lds(w, b[J - PA], base + to + BYTES_A + (wave * PB + J - PA) * 1024);
+      }
+    };
+    // The scales of a chunk of stages from s0 on: A's as [stage][wavefront's rows][16][MI], so that a lane reads those of its rows at once, B's as [block][stage].
+    const auto fill = [&](int s0) {
+      const int n = min(Q8_CHUNK, p.stages - s0);
+      for (int r = tid; r < BM; r += 64 * NW) {
+        const unsigned char* from = p.SA + source(r) * p.stages + s0;
+        lds_char* const to = scales + r / (16 * MI) * (16 * MI) + r % 16 * MI + r / 16 % MI;
+        for (int s = 0; s < n; s += 16) {
+          unsigned v[4];
 #pragma unroll
-        for (int m = 0; m < MI; m++) va[m] = na[m];
-        vw = nw;
-        if (s + 4 < p.stages) {
+          for (int x = 0; x < 4; x++) v[x] = s + 4 * x < n ? q8_scales(from, s + 4 * x, n) : 0;
 #pragma unroll
-          for (int m = 0; m < MI; m++) na[m] = q8_scales(sa[m], s + 4, p.stages);
-          nw = q8_scales(sw, s + 4, p.stages);
+          for (int x = 0; x < 16; x++) to[(s + x) * BM] = (char)(v[x / 4] >> (8 * (x & 3)));
         }
       }
-      q8_traffic<MH, NI>(a, b, now, now, true, false, false, rm + 16 * MH, cn, wave, lane, fa[1], g);
-#pragma unroll
-      for (int m = 0; m < MH; m++)
-#pragma unroll
-        for (int n = 0; n < NI; n++) acc[m][n] = q8_mfma<T>(f[n], fa[0][m], acc[m][n], vw, va[m]);
+      for (int x = tid; x < BLOCKS * Q8_CHUNK; x += 64 * NW) {
+        const int block = min(n0 / Q8_BLOCK + x / Q8_CHUNK, nb - 1), s = min(x % Q8_CHUNK, n - 1);
+        scales[Q8_CHUNK * BM + x] = (char)p.SW[((int64_t)e * nb + block) * p.stages + s0 + s];
+      }
+    };
+    typedef unsigned words __attribute__((ext_vector_type((MI + 3) / 4)));
+    const auto row_scales = [&](int s) -> words {
+      const lds_char* at = scales + (s % Q8_CHUNK) * BM + rm + i * MI;
+      if constexpr (MI == 8) return *(const __attribute__((address_space(3))) words*)at;
+      else if constexpr (MI == 4) return words{*(const __attribute__((address_space(3))) unsigned*)at};
+      else return words{*(const __attribute__((address_space(3))) unsigned short*)at};
+    };
+    const auto col_scale = [&](int s) -> unsigned {
+      return *(const __attribute__((address_space(3))) unsigned char*)(scales + Q8_CHUNK * BM + (n0 % Q8_BLOCK + cn) / Q8_BLOCK * Q8_CHUNK + s % Q8_CHUNK);
+    };
+    const auto fragment = [&](unsigned from, int r0) -> i8v {
+      const lds_char* row = mem + from + (r0 + i) * EMM_STAGE;
+      const u4 lo = *(const __attribute__((address_space(3))) u4*)(row + ((q ^ (i & 7)) * 16)), hi = *(const __attribute__((address_space(3))) u4*)(row + (((4 + q) ^ (i & 7)) * 16));
+      return i8v{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+    };
+    q8_for<PA + PB>([&](auto j) { load(j, 0); });
+    w += EMM_STAGE;
+    if (p.stages > 1) {
+      q8_for<PA + PB>([&](auto j) { load(j, STAGE); });
+      w += EMM_STAGE;
+    }
+    fill(0);
+    const auto meet = [] {  // everything asked for is in LDS, for all wavefronts, and nobody reads any more
       emm_wait<0>();
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      __builtin_amdgcn_s_barrier();  // the next stage is in LDS, and everyone has read this one
+      __builtin_amdgcn_s_barrier();
       asm volatile("" ::: "memory");
-      q8_traffic<MH, NI>(a, b, next, now, s + 1 < p.stages, s + 1 < p.stages, s + 2 < p.stages, rm, cn, wave, lane, fa[0], g);
+    };
+    meet();
+    i8v fa[2], fb[NI];
+    fa[0] = fragment(0, rm);
 #pragma unroll
-      for (int m = 0; m < MH; m++)
-#pragma unroll
-        for (int n = 0; n < NI; n++) acc[MH + m][n] = q8_mfma<T>(f[n], fa[1][m], acc[MH + m][n], vw, va[MH + m]);
-#pragma unroll
-      for (int m = 0; m < MI; m++) va[m] >>= 8;
-      vw >>= 8;
+    for (int n = 0; n < NI; n++) fb[n] = fragment(BYTES_A, cn + 16 * n);
+    words sx = row_scales(0);
+    unsigned sw = col_scale(0);
+    // stage s, in the buffer at `now`; NEXT: there is another one; MORE: and one behind that
+    const auto stage = [&](int s, unsigned now, auto next_, auto more_) {
+      constexpr bool NEXT = decltype(next_)::value, MORE = decltype(more_)::value;
+      const unsigned then = STAGE - now;
+      words nx = sx;
+      unsigned nw = sw;
+      q8_for<MI>([&](auto m_) {
+        constexpr int M = decltype(m_)::value;
+        if constexpr (M + 1 < MI) {
+          fa[(M + 1) & 1] = fragment(now, rm + 16 * (M + 1));
+          __builtin_amdgcn_sched_barrier(0);
+          q8_for<NI>([&](auto n) { acc[M][n.value] = q8_mfma<T, 0, M & 3>(fb[n.value], fa[M & 1], acc[M][n.value], sw, sx[M / 4]); });
+          __builtin_amdgcn_sched_barrier(0);
+        } else {
+          if constexpr (NEXT) {
+            meet();
+            if ((s + 1) % Q8_CHUNK == 0) {
+              fill(s + 1);
+              meet();
+            }
+            nx = row_scales(s + 1);
+            nw = col_scale(s + 1);
+            fa[0] = fragment(then, rm);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+          q8_for<NI>([&](auto n) {
+            constexpr int N = n.value;
+            acc[M][N] = q8_mfma<T, 0, M & 3>(fb[N], fa[M & 1], acc[M][N], sw, sx[M / 4]);
+            if constexpr (NEXT) fb[N] = fragment(then + BYTES_A, cn + 16 * N);
+            if constexpr (MORE) {
+              constexpr int EACH = (PA + PB + NI - 1) / NI;
+              q8_for<EACH>([&](auto x) {
+                if constexpr (N * EACH + x.value < PA + PB) load(Q8Int<N * EACH + x.value>{}, now);
+              });
+            }
+            __builtin_amdgcn_sched_barrier(0);
+          });
+          if constexpr (MORE) w += EMM_STAGE;
+        }
+      });
+      sx = nx;
+      sw = nw;
     };
     int s = 0;
-    for (; s + 1 < p.stages; s += 2) {
-      stage(s, mem, mem + STAGE, fb[0], fb[1]);
-      stage(s + 1, mem + STAGE, mem, fb[1], fb[0]);
+    unsigned now = 0;
+    for (; s + 2 < p.stages; s++) {
+      stage(s, now, std::true_type{}, std::true_type{});
+      now = STAGE - now;
     }
-    if (s < p.stages) stage(s, mem, mem + STAGE, fb[0], fb[1]);
+    if (s + 1 < p.stages) {
+      stage(s, now, std::true_type{}, std::false_type{});
+      now = STAGE - now;
+      s++;
+    }
+    stage(s, now, std::false_type{}, std::false_type{});
   }
   constexpr int PER = Elem<T>::PER16;
   typedef typename Elem<T>::v16 v16;
-  if (p.relu) {
-#pragma unroll
-    for (int m = 0; m < MI; m++)
-#pragma unroll
-      for (int n = 0; n < NI; n++)
-#pragma unroll
-        for (int x = 0; x < 4; x++) acc[m][n][x] = acc[m][n][x] > 0.0f ? acc[m][n][x] : 0.0f;  // (NaN and -0 give +0)
-  }
   emm_store_lines<T, BM, BN, 64 * NW>((lds_char*)lds, acc, rm, cn, [&](int row, int col, v16 v) {
     const int r = m0 + row, c = n0 + col, left = p.NO - c;
     if (r >= hi || left <= 0) return;
     const int64_t o = (int64_t)r * p.NO + c;
     if (p.row && owned && (p.row[r] < 0 || p.row[r] >= p.T)) v = v16{};  // (a row of zeros)
+    if (p.relu) {  // (of what is rounded: the same; NaN and -0 give +0)
+#pragma unroll
+      for (int x = 0; x < PER; x++) v[x] = static_cast<float>(v[x]) > 0.0f ? v[x] : static_cast<T>(0.0f);
+    }
     if (p.gate && owned) {
       const T* const gate = static_cast<const T*>(p.gate) + o;
       Pack<T, PER> h;
@@ -305,7 +353,7 @@ __global__ __launch_bounds__(64 * WK) void expert_few_rows_q8_kernel(Q8Args p) {
       for (int u = 0; u < U; u++)
         if (s + u < last) {
 #pragma unroll
-          for (int n = 0; n < CT; n++) acc[n] = q8_mfma<T>(fb[u][n], fa[u], acc[n], ws[u], xs[u]);
+          for (int n = 0; n < CT; n++) acc[n] = q8_mfma<T, 0, 0>(fb[u][n], fa[u], acc[n], ws[u], xs[u]);
         }
 #pragma unroll
       for (int n = 0; n < CT; n++) b[n] += U * EMM_STAGE;

@@ -4,9 +4,9 @@
 
 namespace tc355 {
 
-// Side of the (square) tile.
-inline int q8_tile_side(int cus, int64_t R, int64_t E, int64_t NO) {
-  return expert_tile_side(128, cus, [&](int b) { return expected_row_tiles(R, E, b) * (double)ceil_div(NO, b); });
+// Side of the (square) tile.  Products of float outputs, which go by the half instruction, take 128 at most.
+inline int q8_tile_side(bool f32, int cus, int64_t R, int64_t E, int64_t NO) {
+  return expert_tile_side(f32 ? 128 : 256, cus, [&](int b) { return expected_row_tiles(R, E, b) * (double)ceil_div(NO, b); });
 }
 
 // Whether a product goes to the kernel for few rows rather than to tiles.
