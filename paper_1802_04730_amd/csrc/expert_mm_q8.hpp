@@ -108,16 +108,18 @@ __device__ __forceinline__ void q8_to_lds(const char* base, unsigned off, unsign
 
 constexpr int Q8_CHUNK = 64;  // stages whose scales are in LDS
 
-// Each wavefront multiplies MI x NI blocks of 16 x 16, a stage in MI steps.  A step multiplies one block of 16 rows with all columns while the next block's fragment is
-// read.  Before the last step a barrier: the next stage is in LDS, and nobody reads this one any more; so the last step replaces each column's fragment by the next stage's, as soon as it
-// is used, and requests the stage after that.  Four wavefronts: 128 x 128 of a tile of 256 each read a third less from LDS (128 KB a stage) than eight, whose
-// reads and the loads' writes would take as long as the products; a wavefront has all 512 registers of its SIMD's lanes, half of them sums.
+// Each wavefront multiplies MI x NI blocks of 16 x 16, a stage in MI steps: a step multiplies one block of 16 rows with all columns.  The first half of the steps reads the other rows'
+// fragments; then a barrier: nobody reads this buffer any more, and the second half requests the stage after the next into it, a few loads a step, since the wavefront
+// stands still where the address path has more than it takes.  Before the last step another barrier: the next stage, requested a stage and a half before, is in LDS, and the
+// last step replaces each column's fragment by the next stage's as soon as it is used.  Four wavefronts: 128 x 128 of a tile of 256 each read a third less from LDS (128 KB a
+// stage) than eight, whose reads and the loads' writes would take as long as the products; a wavefront has all 512 registers of its SIMD's lanes, half of them sums.
 template <typename T, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(64 * WM * WN) void expert_mm_q8_kernel(Q8Args p) {
   constexpr int NW = WM * WN, MI = BM / WM / 16, NI = BN / WN / 16;
-  constexpr int PA = BM / 8 / NW, PB = BN / 8 / NW;  // loads of a wavefront a stage, 8 rows each
+  constexpr int PA = BM / 8 / NW, PB = BN / 8 / NW, LOADS = PA + PB;  // loads of a wavefront a stage, 8 rows each
+  constexpr int EACH = LOADS / (MI / 2);                              // of them in each of the steps of a stage's second half
   constexpr int BLOCKS = (BN + Q8_BLOCK - 1) / Q8_BLOCK;
-  static_assert(MI % 2 == 0 && PA * 8 * NW == BM && PB * 8 * NW == BN && BN / WN <= Q8_BLOCK, "whole steps, loads and blocks");
+  static_assert(MI % 2 == 0 && EACH * (MI / 2) == LOADS && PA * 8 * NW == BM && PB * 8 * NW == BN && BN / WN <= Q8_BLOCK, "whole steps, loads and blocks");
   constexpr int BYTES_A = BM * EMM_STAGE, STAGE = (BM + BN) * EMM_STAGE;
   constexpr int SCALES = Q8_CHUNK * (BM + BLOCKS), OUT = BM * BN * sizeof(T);
   __shared__ __align__(16) char lds[2 * STAGE + SCALES > OUT ? 2 * STAGE + SCALES : OUT];
@@ -195,21 +197,22 @@ __global__ __launch_bounds__(64 * WM * WN) void expert_mm_q8_kernel(Q8Args p) {
       const u4 lo = *(const __attribute__((address_space(3))) u4*)(row + ((q ^ (i & 7)) * 16)), hi = *(const __attribute__((address_space(3))) u4*)(row + (((4 + q) ^ (i & 7)) * 16));
       return i8v{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
     };
-    q8_for<PA + PB>([&](auto j) { load(j, 0); });
+    q8_for<LOADS>([&](auto j) { load(j, 0); });
     w += EMM_STAGE;
     if (p.stages > 1) {
-      q8_for<PA + PB>([&](auto j) { load(j, STAGE); });
+      q8_for<LOADS>([&](auto j) { load(j, STAGE); });
       w += EMM_STAGE;
     }
     fill(0);
-    const auto meet = [] {  // everything asked for is in LDS, for all wavefronts, and nobody reads any more
-      emm_wait<0>();
+    // All but the last `left_` loads are in LDS, for all wavefronts, and what any of them has asked LDS for is there.
+    const auto meet = [](auto left_) {
+      emm_wait<decltype(left_)::value>();
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       __builtin_amdgcn_s_barrier();
       asm volatile("" ::: "memory");
     };
-    meet();
-    i8v fa[2], fb[NI];
+    meet(Q8Int<0>{});
+    i8v fa[MI], fb[NI];
     fa[0] = fragment(0, rm);
 #pragma unroll
     for (int n = 0; n < NI; n++) fb[n] = fragment(BYTES_A, cn + 16 * n);
@@ -222,39 +225,38 @@ __global__ __launch_bounds__(64 * WM * WN) void expert_mm_q8_kernel(Q8Args p) {
       words nx = sx;
       unsigned nw = sw;
       q8_for<MI>([&](auto m_) {
-        constexpr int M = decltype(m_)::value;
-        if constexpr (M + 1 < MI) {
-          fa[(M + 1) & 1] = fragment(now, rm + 16 * (M + 1));
-          __builtin_amdgcn_sched_barrier(0);
-          q8_for<NI>([&](auto n) { acc[M][n.value] = q8_mfma<T, 0, M & 3>(fb[n.value], fa[M & 1], acc[M][n.value], sw, sx[M / 4]); });
-          __builtin_amdgcn_sched_barrier(0);
-        } else {
-          if constexpr (NEXT) {
-            meet();
-            if ((s + 1) % Q8_CHUNK == 0) {
-              fill(s + 1);
-              meet();
-            }
-            nx = row_scales(s + 1);
-            nw = col_scale(s + 1);
-            fa[0] = fragment(then, rm);
-          }
-          __builtin_amdgcn_sched_barrier(0);
-          q8_for<NI>([&](auto n) {
-            constexpr int N = n.value;
-            acc[M][N] = q8_mfma<T, 0, M & 3>(fb[N], fa[M & 1], acc[M][N], sw, sx[M / 4]);
-            if constexpr (NEXT) fb[N] = fragment(then + BYTES_A, cn + 16 * N);
-            if constexpr (MORE) {
-              constexpr int EACH = (PA + PB + NI - 1) / NI;
-              q8_for<EACH>([&](auto x) {
-                if constexpr (N * EACH + x.value < PA + PB) load(Q8Int<N * EACH + x.value>{}, now);
-              });
-            }
-            __builtin_amdgcn_sched_barrier(0);
-          });
-          if constexpr (MORE) w += EMM_STAGE;
+        constexpr int M = decltype(m_)::value, H = MI / 2;
+        if constexpr (M < H) {
+          fa[2 * M + 1] = fragment(now, rm + 16 * (2 * M + 1));
+          if constexpr (2 * M + 2 < MI) fa[2 * M + 2] = fragment(now, rm + 16 * (2 * M + 2));
         }
+        if constexpr (M == H && M + 1 < MI && MORE) meet(Q8Int<LOADS>{});  // (the next stage may be on its way still)
+        if constexpr (M + 1 == MI && NEXT) {
+          meet(Q8Int<MORE ? EACH * (H - 1) : 0>{});
+          if ((s + 1) % Q8_CHUNK == 0) {
+            fill(s + 1);
+            meet(Q8Int<0>{});
+          }
+          nx = row_scales(s + 1);
+          nw = col_scale(s + 1);
+          fa[0] = fragment(then, rm);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        q8_for<NI>([&](auto n_) {
+          constexpr int N = decltype(n_)::value;
+          acc[M][N] = q8_mfma<T, 0, M & 3>(fb[N], fa[M], acc[M][N], sw, sx[M / 4]);
+          if constexpr (M + 1 == MI && NEXT) fb[N] = fragment(then + BYTES_A, cn + 16 * N);
+          if constexpr (M >= H && MORE) {
+            constexpr int FIRST = (M - H) * EACH;  // of this step's loads; one behind each NI / EACH columns
+            q8_for<EACH>([&](auto x) {
+              if constexpr (x.value * NI / EACH == N) load(Q8Int<FIRST + x.value>{}, now);
+            });
+          }
+          if constexpr (M >= H) __builtin_amdgcn_sched_barrier(0);
+        });
+        __builtin_amdgcn_sched_barrier(0);
       });
+      if constexpr (MORE) w += EMM_STAGE;
       sx = nx;
       sw = nw;
     };
