@@ -4,16 +4,36 @@
 
 namespace tc355 {
 
-// Side of the (square) tile.  Products of float outputs, which go by the half instruction, take 128 at most.
-inline int q8_tile_side(bool f32, int cus, int64_t R, int64_t E, int64_t NO) {
-  return expert_tile_side(f32 ? 128 : 256, cus, [&](int b) { return expected_row_tiles(R, E, b) * (double)ceil_div(NO, b); });
+// Side of the (square) tile: the estimate is a compute unit's number of tiles times a tile's products, over the rate that the side reaches relative to the others, and as
+// many stages more as a tile's start and end take.  float outputs (by the half instruction) take 128 at most.  Measured, operands in 8 bits, bfloat16, us, sides 64 / 128 / 256:
+// (E,R,N,K) = (1,4096,8192,4096) 204 / 133 / 125, of K = 1024 63 / 44 / 49, uneven shares (32,16384,2048,4096) 291 / 225 / 224, (32,16384,4096,2048) 331 / 256 / 287,
+// (8,8192,1024,4096) 71 / 58 / 60, (64,4096,1024,1024) 20 / 17 / 25, (16,2048,2048,2048) 26 / 19 / 31, (64,2048,1024,2048) 24 / 26 / 39, (1,512,4096,4096) 21 / 28 / 54,
+// (4,2000,512,512) 5.3 / 7.0 / 14; float, sides 64 / 128: (1,4096,4096,4096) 216 / 183, (32,8192,2048,2048) 146 / 128, (16,2048,2048,2048) 39 / 47, (12,2100,1001,517) 12 / 17.
+inline int q8_tile_side(bool f32, int cus, int64_t R, int64_t E, int64_t NO, int64_t stages) {
+  const struct {
+    int side;
+    double rate, more;
+  } sides[] = {{256, f32 ? 0 : 1.0, 2}, {128, f32 ? 1.0 : 0.95, 1}, {64, f32 ? 0.85 : 0.62, 0.5}};
+  int best = 0;
+  double least = 0;
+  for (const auto& s : sides) {
+    if (s.rate == 0) continue;
+    const double load = expected_row_tiles(R, E, s.side) * (double)ceil_div(NO, s.side) / cus;
+    const double t = (load < 1 ? 1 : load) * s.side * s.side / s.rate * (1 + s.more / (double)stages);
+    if (!best || t < least) {
+      best = s.side;
+      least = t;
+    }
+  }
+  return best;
 }
 
-// Whether a product goes to the kernel for few rows rather than to tiles.
-inline bool q8_few_rows(int cus, int64_t R, int64_t E, int64_t NO) {
-  if (R / E >= 64) return false;
-  const double few = expected_row_tiles(R, E, 16) * ceil_div(NO, 32) / cus, tile = expected_row_tiles(R, E, 64) * ceil_div(NO, 64) / cus;
-  return 1 + 1.5 * (few > 0.5 ? few - 0.5 : 0) <= 4.5 + (tile > 0.5 ? tile - 0.5 : 0);
+// Whether a product goes to the kernel for few rows (16 rows by 32 columns a workgroup, the reduction shared by its wavefronts) rather than to tiles of 64: while it has up to two
+// workgroups a compute unit (three for float).  Beyond, tiles read the rows' share of the operands less often.  Measured, us, few / tiles: (1,1,8192,4096) 7.5 / 18, 16 rows 9.9 / 19, 33 rows 20 / 19,
+// 63 rows 27 / 20; (1,32,2048,8192) 16 / 23; (1,100,512,4096) 9.0 / 13; (8,8,1024,4096) 8.0 / 13; (8,32,4096,2048) 14.3 / 14.0, float 16 / 21; (8,128,4096,2048) 22 / 14;
+// (32,128,2048,1024) 24 / 13; (1,16,4096,1024) 5.5 / 5.2.
+inline bool q8_few_rows(bool f32, int cus, int64_t R, int64_t E, int64_t NO) {
+  return expected_row_tiles(R, E, 16) * (double)ceil_div(NO, 32) <= (f32 ? 3.0 : 2.0) * cus;
 }
 
 }  // namespace tc355

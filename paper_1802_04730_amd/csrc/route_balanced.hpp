@@ -143,15 +143,15 @@ __global__ __launch_bounds__(WG_THREADS) void route_balanced_kernel(RouteBalance
         }
       const unsigned upper = (unsigned)(mine >> 32), best = group_all<G>(upper, larger);
       const unsigned long long agree = __ballot(upper == best);
-      const unsigned within = G == 64 ? 0 : (threadIdx.x & 63) & ~(G - 1);
-      const unsigned long long members = G == 64 ? agree : agree >> within & ((1ull << G) - 1);
+      const unsigned within = (threadIdx.x & 63) & ~(G - 1);
+      const unsigned long long members = agree >> within & (~0ull >> (64 - G));
       bool winner = upper == best;
       if (members & (members - 1)) {  // (several: by the lower halves, then by the lane, whose experts come first)
         const unsigned lower = winner ? (unsigned)mine : 0, low = group_all<G>(lower, larger);
         winner = winner && lower == low;
       }
       const unsigned long long last = __ballot(winner);
-      const int src = __ffsll((long long)(G == 64 ? last : last >> within & ((1ull << G) - 1))) - 1;
+      const int src = __ffsll((long long)(last >> within & (~0ull >> (64 - G)))) - 1;
       float chosen = 0;
 #pragma unroll
       for (int v = 0; v < V; v++)

@@ -326,11 +326,11 @@ tc_status tc_expert_mm_q8(const void* X, const void* SX, const void* W, const vo
     a.SA = bytes(workspace) + pl.scales;
     if (const tc_status st = quantize_rows(X, workspace, static_cast<char*>(workspace) + pl.scales, T, K, type, s); st != TC_OK) return st;
   }
-  const bool few = q8_few_rows(compute_units(), R, E, N);
+  const bool few = q8_few_rows(type == TC_F32, compute_units(), R, E, N);
   return took(few ? "expert_mm_q8:rows" : "expert_mm_q8:tile", by_type(type, [&](auto t) {
                 typedef decltype(t) X_;
                 if (few) return launch_q8_few<X_, 2, 4>(a, s);
-                const int side = q8_tile_side(type == TC_F32, compute_units(), R, E, N);
+                const int side = q8_tile_side(type == TC_F32, compute_units(), R, E, N, a.stages);
                 if constexpr (sizeof(X_) == 2)
                   if (side == 256) return launch_q8_tile<X_, 256, 2, 2>(a, s);
                 return side == 64 ? launch_q8_tile<X_, 64, 2, 2>(a, s) : launch_q8_tile<X_, 128, 2, 2>(a, s);
