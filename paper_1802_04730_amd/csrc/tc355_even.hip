@@ -247,7 +247,7 @@ tc_status tc_route_balanced(const void* L, const float* Bias, float* Wt, int32_t
   return by_type(type, [&](auto x) {
     return by_lanes(E, k, [&](auto g, auto v) {
       typedef decltype(x) X;
-      const size_t scores = keep < groups ? (size_t)(WG_THREADS / g.value) * (E + groups) * 8 : 0;
+      const size_t scores = keep < groups ? (size_t)(WG_THREADS / g.value) * score_places((int)E, (int)groups) * 8 : 0;
       route_balanced_kernel<X, g.value, v.value><<<dim3((unsigned)a.r.tiles), dim3(WG_THREADS), (a.r.count ? bins : bins * (1 + WAVES_PER_WG)) + scores, s>>>(a);
       if (!a.r.count) return took("route_balanced:one", launched());
       if (a.r.summed) sort_sum_kernel<<<dim3(1u << a.r.bits), dim3(WG_THREADS), 0, s>>>(a.r.count, a.r.tiles);
