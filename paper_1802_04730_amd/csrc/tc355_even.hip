@@ -62,8 +62,8 @@ tc_status by_norm_types(tc_type type, tc_type weight, F f) {
   return by_type(type, [&](auto t) { return weight == TC_F32 ? f(t, float{}) : f(t, t); });
 }
 
-// Parts of the sums for dW and dB: at least 16 rows each.
-int64_t norm_parts(int64_t T) { return std::min<int64_t>(ceil_div(T, 16), NORM_MOST_PARTS); }
+// Parts of the sums for dW and dB.
+int64_t norm_parts(int64_t T) { return std::min<int64_t>(T, NORM_MOST_PARTS); }
 struct NormPlan {
   int64_t parts, stat, bytes;
 };
