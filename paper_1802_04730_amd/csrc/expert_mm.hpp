@@ -506,10 +506,10 @@ __device__ __forceinline__ void emm_store(TO* p, int left, bool whole, f4 v) {
 // A tile of results by whole lines: through LDS (16-byte chunk c of row r in slot c ^ (r & 7)), then 16 bytes a lane, neighbours along the
 // row, past the caches.  put(row, column, values): stores 16 bytes of the tile.  (The accumulators' own pieces of 8 or 16 bytes: the
 // gradient of the weights of (E,R,N,K) = (32,16384,2048,4096) in bfloat16 486 us instead of 395, 8192^3 forward 863 instead of 785.)
-template <typename TO, int BM, int BN, int THREADS, int MI, int NI, typename Put>
-__device__ __forceinline__ void emm_store_lines(lds_char* lds, const f4 (&acc)[MI][NI], int rm, int cn, Put put) {
+template <typename TO, int BN, int MI, int NI>
+__device__ __forceinline__ void emm_lines_to_lds(lds_char* lds, const f4 (&acc)[MI][NI], int rm, int cn) {
   constexpr int PER = Elem<TO>::PER16, ROW = BN * sizeof(TO);
-  const int tid = threadIdx.x, lane = tid & 63, i = lane & 15, q = lane >> 4;
+  const int lane = threadIdx.x & 63, i = lane & 15, q = lane >> 4;
   typedef typename Elem<TO>::v4 v4;
   __syncthreads();  // (everyone has read the last stage)
 #pragma unroll
@@ -523,12 +523,20 @@ __device__ __forceinline__ void emm_store_lines(lds_char* lds, const f4 (&acc)[M
       *(__attribute__((address_space(3))) v4*)(lds + r * ROW + (((c / PER) ^ (r & 7)) * 16) + c % PER * (int)sizeof(TO)) = o;
     }
   __syncthreads();
+}
+// Chunk x of the tile, of BN / PER16 a row.
+template <typename TO, int BN>
+__device__ __forceinline__ typename Elem<TO>::v16 emm_line(const lds_char* lds, int x) {
+  constexpr int PER = Elem<TO>::PER16, ROW = BN * sizeof(TO);
+  const int r = x / (BN / PER), c = x % (BN / PER);
+  return __builtin_bit_cast(typename Elem<TO>::v16, *(const __attribute__((address_space(3))) u4*)(lds + r * ROW + ((c ^ (r & 7)) * 16)));
+}
+template <typename TO, int BM, int BN, int THREADS, int MI, int NI, typename Put>
+__device__ __forceinline__ void emm_store_lines(lds_char* lds, const f4 (&acc)[MI][NI], int rm, int cn, Put put) {
+  constexpr int PER = Elem<TO>::PER16;
+  emm_lines_to_lds<TO, BN>(lds, acc, rm, cn);
 #pragma unroll 4
-  for (int x = tid; x < BM * BN / PER; x += THREADS) {
-    const int r = x / (BN / PER), c = x % (BN / PER);
-    const u4 v = *(const __attribute__((address_space(3))) u4*)(lds + r * ROW + ((c ^ (r & 7)) * 16));
-    put(r, PER * c, __builtin_bit_cast(typename Elem<TO>::v16, v));
-  }
+  for (int x = threadIdx.x; x < BM * BN / PER; x += THREADS) put(x / (BN / PER), PER * (x % (BN / PER)), emm_line<TO, BN>(lds, x));
 }
 
 // ---- kernels ---------------------------------------------------------------------------------------------------------------

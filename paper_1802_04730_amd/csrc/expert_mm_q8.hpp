@@ -275,36 +275,67 @@ __global__ __launch_bounds__(64 * WM * WN) void expert_mm_q8_kernel(Q8Args p) {
   }
   constexpr int PER = Elem<T>::PER16;
   typedef typename Elem<T>::v16 v16;
-  emm_store_lines<T, BM, BN, 64 * NW>((lds_char*)lds, acc, rm, cn, [&](int row, int col, v16 v) {
-    const int r = m0 + row, c = n0 + col, left = p.NO - c;
-    if (r >= hi || left <= 0) return;
-    const int64_t o = (int64_t)r * p.NO + c;
-    if (p.row && owned && (p.row[r] < 0 || p.row[r] >= p.T)) v = v16{};  // (a row of zeros)
-    if (p.relu) {  // (of what is rounded: the same; NaN and -0 give +0)
+  emm_lines_to_lds<T, BN>((lds_char*)lds, acc, rm, cn);
+  const auto clamped = [&](v16 v, bool nothing, const Pack<T, PER>& gate) {
 #pragma unroll
-      for (int x = 0; x < PER; x++) v[x] = static_cast<float>(v[x]) > 0.0f ? v[x] : static_cast<T>(0.0f);
+    for (int x = 0; x < PER; x++) {
+      if (nothing) v[x] = static_cast<T>(0.0f);  // (a row of zeros)
+      if (p.relu) v[x] = static_cast<float>(v[x]) > 0.0f ? v[x] : static_cast<T>(0.0f);  // (of what is rounded: the same; NaN and -0 give +0)
+      if (p.gate && owned) v[x] = static_cast<float>(gate.e[x]) > 0.0f ? v[x] : static_cast<T>(0.0f);
     }
-    if (p.gate && owned) {
-      const T* const gate = static_cast<const T*>(p.gate) + o;
-      Pack<T, PER> h;
-      if (left >= PER) {
-        h = load_pack<T, PER>(gate);
-      } else {
+    return v;
+  };
+  constexpr int CHUNKS = BM * BN / PER, EACH_THREAD = CHUNKS / (64 * NW), U = EACH_THREAD < 8 ? EACH_THREAD : 8;
+  if (p.NO % PER == 0) {  // U chunks at a time, whose gates and rows are asked for together
+    const auto batch = [&](int j0, auto gated) {
+      Pack<T, PER> gate[U];
+      int row[U], src[U], col[U];
 #pragma unroll
-        for (int x = 0; x < PER; x++) h.e[x] = x < left ? gate[x] : static_cast<T>(0.0f);
+      for (int u = 0; u < U; u++) {
+        const int x = tid + (j0 + u) * 64 * NW;
+        row[u] = m0 + x / (BN / PER);
+        col[u] = n0 + x % (BN / PER) * PER;
+        const int r = min(row[u], hi - 1);  // (past the end: any that is there)
+        src[u] = p.row && owned ? p.row[r] : 0;
+        if constexpr (gated.value) gate[u] = load_pack<T, PER>(static_cast<const T*>(p.gate) + (int64_t)r * p.NO + min(col[u], p.NO - PER));
       }
 #pragma unroll
-      for (int x = 0; x < PER; x++) v[x] = static_cast<float>(h.e[x]) > 0.0f ? v[x] : static_cast<T>(0.0f);
+      for (int u = 0; u < U; u++) {
+        const v16 v = clamped(emm_line<T, BN>((lds_char*)lds, tid + (j0 + u) * 64 * NW), src[u] < 0 || (src[u] >= p.T && owned), gate[u]);
+        if (row[u] < hi && col[u] < p.NO) __builtin_nontemporal_store(v, reinterpret_cast<v16*>(static_cast<T*>(p.C) + (int64_t)row[u] * p.NO + col[u]));
+      }
+    };
+    if (p.gate && owned) {
+      for (int j0 = 0; j0 < EACH_THREAD; j0 += U) batch(j0, std::true_type{});
+    } else {
+      for (int j0 = 0; j0 < EACH_THREAD; j0 += U) batch(j0, std::false_type{});
     }
+    return;
+  }
+  for (int x = tid; x < CHUNKS; x += 64 * NW) {
+    const int r = m0 + x / (BN / PER), c = n0 + x % (BN / PER) * PER, left = p.NO - c;
+    if (r >= hi || left <= 0) continue;
+    const int64_t o = (int64_t)r * p.NO + c;
+    Pack<T, PER> gate{};
+    if (p.gate && owned) {
+      const T* const g = static_cast<const T*>(p.gate) + o;
+      if (left >= PER) {
+        gate = load_pack<T, PER>(g);
+      } else {
+#pragma unroll
+        for (int y = 0; y < PER; y++) gate.e[y] = y < left ? g[y] : static_cast<T>(0.0f);
+      }
+    }
+    const v16 v = clamped(emm_line<T, BN>((lds_char*)lds, x), p.row && owned && (p.row[r] < 0 || p.row[r] >= p.T), gate);
     T* const out = static_cast<T*>(p.C) + o;
     if (left >= PER) {
       store_pack<T, PER>(out, __builtin_bit_cast(Pack<T, PER>, v));
     } else {
 #pragma unroll
-      for (int x = 0; x < PER; x++)
-        if (x < left) out[x] = v[x];
+      for (int y = 0; y < PER; y++)
+        if (y < left) out[y] = v[y];
     }
-  });
+  }
 }
 
 // Few rows an expert (a decoding step): 16 rows by 16 CT columns a workgroup, whose wavefronts share the reduction; operands go from memory to registers in the
