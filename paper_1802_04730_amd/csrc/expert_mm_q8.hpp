@@ -276,12 +276,15 @@ __global__ __launch_bounds__(64 * WM * WN) void expert_mm_q8_kernel(Q8Args p) {
   constexpr int PER = Elem<T>::PER16;
   typedef typename Elem<T>::v16 v16;
   emm_lines_to_lds<T, BN>((lds_char*)lds, acc, rm, cn);
-  const auto clamped = [&](v16 v, bool nothing, const Pack<T, PER>& gate) {
+  const auto clamped = [&](v16 v, bool nothing, auto gated, const Pack<T, PER>& gate) {
+    if (nothing) v = v16{};  // (a row of zeros)
+    if (p.relu) {  // (of what is rounded: the same; NaN and -0 give +0)
 #pragma unroll
-    for (int x = 0; x < PER; x++) {
-      if (nothing) v[x] = static_cast<T>(0.0f);  // (a row of zeros)
-      if (p.relu) v[x] = static_cast<float>(v[x]) > 0.0f ? v[x] : static_cast<T>(0.0f);  // (of what is rounded: the same; NaN and -0 give +0)
-      if (p.gate && owned) v[x] = static_cast<float>(gate.e[x]) > 0.0f ? v[x] : static_cast<T>(0.0f);
+      for (int x = 0; x < PER; x++) v[x] = static_cast<float>(v[x]) > 0.0f ? v[x] : static_cast<T>(0.0f);
+    }
+    if constexpr (decltype(gated)::value) {
+#pragma unroll
+      for (int x = 0; x < PER; x++) v[x] = static_cast<float>(gate.e[x]) > 0.0f ? v[x] : static_cast<T>(0.0f);
     }
     return v;
   };
@@ -301,7 +304,7 @@ __global__ __launch_bounds__(64 * WM * WN) void expert_mm_q8_kernel(Q8Args p) {
       }
 #pragma unroll
       for (int u = 0; u < U; u++) {
-        const v16 v = clamped(emm_line<T, BN>((lds_char*)lds, tid + (j0 + u) * 64 * NW), src[u] < 0 || (src[u] >= p.T && owned), gate[u]);
+        const v16 v = clamped(emm_line<T, BN>((lds_char*)lds, tid + (j0 + u) * 64 * NW), src[u] < 0 || (src[u] >= p.T && owned), gated, gate[u]);
         if (row[u] < hi && col[u] < p.NO) __builtin_nontemporal_store(v, reinterpret_cast<v16*>(static_cast<T*>(p.C) + (int64_t)row[u] * p.NO + col[u]));
       }
     };
@@ -326,7 +329,9 @@ __global__ __launch_bounds__(64 * WM * WN) void expert_mm_q8_kernel(Q8Args p) {
         for (int y = 0; y < PER; y++) gate.e[y] = y < left ? g[y] : static_cast<T>(0.0f);
       }
     }
-    const v16 v = clamped(emm_line<T, BN>((lds_char*)lds, x), p.row && owned && (p.row[r] < 0 || p.row[r] >= p.T), gate);
+    const bool nothing = p.row && owned && (p.row[r] < 0 || p.row[r] >= p.T);
+    const v16 line = emm_line<T, BN>((lds_char*)lds, x);
+    const v16 v = p.gate && owned ? clamped(line, nothing, std::true_type{}, gate) : clamped(line, nothing, std::false_type{}, gate);
     T* const out = static_cast<T*>(p.C) + o;
     if (left >= PER) {
       store_pack<T, PER>(out, __builtin_bit_cast(Pack<T, PER>, v));
