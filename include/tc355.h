@@ -7,7 +7,8 @@
  * on the right-hand side, of a product of tensor accesses, optionally followed
  * by a pointwise epilogue.  This library evaluates six fixed comprehensions,
  * and the operators around the experts of a language model (tc_embed to
- * tc_expert_sum_grad, whose tensors may be of 16 bits) with their gradients.
+ * tc_expert_mm_q8, whose tensors may be of 16 bits, weights and rows of
+ * products of 8) with their gradients.
  *
  * Conventions common to every entry point
  *  - Every tensor pointer is a DEVICE pointer to a dense row-major array (last

@@ -5,13 +5,20 @@
 //
 // Tiles, stages of 128 bytes, their way to LDS and the swizzle are expert_mm.hpp's.  A stage is a block of 128 elements: one matrix instruction of 16 x 16 x 128
 // takes a whole stage, with the scales' bytes as operands, so that scaling costs nothing.  A lane's 32 bytes of a row are the chunks q and 4 + q: which elements those are is
-// all the same, as long as both operands agree.  While one half of a wavefront's rows is multiplied, the other half's fragments are read.
+// all the same, as long as both operands agree.
 //
 // The 8-bit matrix instruction adds the products of 8 neighbours with the bits down to 2^-13 of the largest one's exponent and cuts the rest; beyond these
 // groups its sums keep 24 bits (measured with products that cancel).  So up to 2^-10 of a group's largest product is lost -- operands in e4m3 are
 // off by 2^-4 of their own --, a choice for 16-bit outputs, whose rounding is as coarse (2^-16 of an output's norm with normally distributed operands; bfloat16 keeps 2^-9): its rate is over
 // three times the 16-bit instruction's (3.8 PFLOP/s against 1.2, both from registers).  float outputs go by the half instruction instead, which takes the same
 // values, widened, and sums them in 32 bits.
+//
+// Measured, rows and weights in 8 bits, bfloat16: (R,N,K) = (4096,8192,4096) 125-131 us (2.1-2.2 PFLOP/s; the library's product without blocks 95), 8192^3 460 (2.4), (4096,4096,8192) 109
+// (2.5); 32 experts, 16384 rows, uneven shares, 2048 x 4096 203, the gradient of the rows with a gate 223; eight experts with 4 rows each, 4096 x 2048, 14 (4.8 TB/s of weights).  A stage of a tile
+// of 256 takes 1.4 us where few tiles run and 1.5-1.7 where all do; its products alone 0.87, or 1.2 at the power that 256 compute units may draw.  What is left are the loads: 0.3 us a stage,
+// as four wavefronts ask the address path at once, whether LDS is read or not, and 0.1 for two barriers.  Tried and left: a branch behind each matrix instruction that gives every wavefront slots of its
+// own for its loads (2.6 us a stage), a copy of the loop for each wavefront instead (1.6), eight wavefronts (1.4 / 1.7), loads spread over the next stage's first steps too (1.5 / 1.7), buffer
+// loads (the same); rows put in 8 bits by the kernel for few rows itself (22 us where the launch before it and the product take 18).
 #pragma once
 #include "expert_mm.hpp"
 #include "quantize8.hpp"

@@ -12,6 +12,10 @@
 // go through LDS once: lane g finds the two best of group g, and ranks it by counting the better ones.  Then k rounds find the largest of what is left, by keys of 32 bits
 // made of the score and the expert's number; where these do not tell two scores apart that differ, the wavefront chooses again by 64 bits.  The scores of the k
 // chosen are computed again by the lanes that write them, all at once.  What bounds it is the rounds' latency and the exponentials of 64 bits.
+//
+// Measured: 16384 tokens of 256 experts, 16 groups of which 5, 8 chosen, 28-32 us for the selection (43 with k rounds over keys of 64 bits, library exponentials and scores at a stride of
+// 128 bytes in LDS; of it 8 for the rounds, 3 for the groups), 12 for sums and places, 7-8 for the gradient; tc_route, with as many lanes a token, takes 48 for all but the gradient.
+// 16 tokens of 128, 8 groups of which 3, 6 chosen, 9.7 in one launch (7.4 with one chosen and no groups).
 #pragma once
 #include "expert_types.hpp"
 #include "lanes.hpp"

@@ -740,7 +740,7 @@ const char* tc_status_string(tc_status s) {
   return "unknown tc_status";
 }
 
-int tc355_version(void) { return 300; }
+int tc355_version(void) { return 400; }
 
 tc_status tc355_set_option(tc_option key, int64_t value) {
   switch (key) {
