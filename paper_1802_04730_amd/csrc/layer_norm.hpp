@@ -11,7 +11,8 @@
 // read X anyway.  Sums over the rows: each workgroup's own, in its order of the rows, are joined in the workgroups' order by a second launch; no
 // atomics.  Rows too long for registers (norm_long_*) are read once for each sum; their dW and dB come from a pass down the columns.
 //
-// Sums are in 32 bits for 16-bit storage and in 64 for float storage, as everywhere where rows are only streamed.
+// Sums are in 32 bits for 16-bit storage and in 64 for float storage, as everywhere where rows are only streamed; along rows too long for registers in 64, since a lane adds up to
+// 2^18 elements of one: in 32 bits, squares of one size would be off by parts in 2^8.
 //
 // Measured: 16384 rows of 4096 bfloat16, weights in float, 51-53 us (5.1-5.2 TB/s) forward, 87-92 for the gradient (4.6) and 6.5 for its join; 8 rows of 2048 4.2; 1500 rows of 333 floats
 // 3.8, 7.9 and 4.5 (16 rows a part, four a group of lanes: 10.5 and 3).
@@ -222,29 +223,34 @@ template <int V, typename F>
 __device__ __forceinline__ void norm_units(int N, F f) {
   for (int64_t x = threadIdx.x; x * V < N; x += WG_THREADS) f(RowUnit<V>(x, N));
 }
+// (the neighbours of a unit are added in S, units in 64 bits)
 template <typename T, int V, typename S>
-__device__ __forceinline__ void norm_long_stats(const T* row, int N, S eps, S* lds, int& turn, S* mean, S* inverse) {
-  S sum = 0;
+__device__ __forceinline__ void norm_long_stats(const T* row, int N, S eps, double* lds, int& turn, S* mean, S* inverse) {
+  double sum = 0;
   norm_units<V>(N, [&](const RowUnit<V>& u) {
     const Pack<T, V> x = load_unit<T, V>(row, u);
+    S of = 0;
 #pragma unroll
-    for (int i = 0; i < V; i++) sum += i >= u.skip ? (S)x.e[i] : (S)0;
+    for (int i = 0; i < V; i++) of += i >= u.skip ? (S)x.e[i] : (S)0;
+    sum += of;
   });
-  const S m = norm_sum<WG_THREADS>(sum, lds, turn) / (S)N;
-  S square = 0;
+  const S m = (S)(norm_sum<WG_THREADS>(sum, lds, turn) / N);
+  double square = 0;
   norm_units<V>(N, [&](const RowUnit<V>& u) {
     const Pack<T, V> x = load_unit<T, V>(row, u);
+    S of = 0;
 #pragma unroll
-    for (int i = 0; i < V; i++) square += i >= u.skip ? ((S)x.e[i] - m) * ((S)x.e[i] - m) : (S)0;
+    for (int i = 0; i < V; i++) of += i >= u.skip ? ((S)x.e[i] - m) * ((S)x.e[i] - m) : (S)0;
+    square += of;
   });
   *mean = m;
-  *inverse = norm_inverse(norm_sum<WG_THREADS>(square, lds, turn) / (S)N + eps);
+  *inverse = norm_inverse((S)(norm_sum<WG_THREADS>(square, lds, turn) / N) + eps);
 }
 
 template <typename T, typename TW, int V>
 __global__ __launch_bounds__(WG_THREADS) void norm_long_kernel(NormArgs p) {
   typedef typename Wide<T>::type S;
-  __shared__ S lds[8];
+  __shared__ double lds[8];
   int turn = 0;
   for (int64_t t = blockIdx.x; t < p.T; t += gridDim.x) {
     const T* row = static_cast<const T*>(p.X) + t * p.N;
@@ -266,28 +272,31 @@ __global__ __launch_bounds__(WG_THREADS) void norm_long_kernel(NormArgs p) {
 template <typename T, typename TW, int V>
 __global__ __launch_bounds__(WG_THREADS) void norm_long_grad_kernel(NormArgs p) {
   typedef typename Wide<T>::type S;
-  __shared__ S lds[8];
+  __shared__ double lds[8];
   int turn = 0;
   for (int64_t t = blockIdx.x; t < p.T; t += gridDim.x) {
     const T *row = static_cast<const T*>(p.X) + t * p.N, *grad = static_cast<const T*>(p.dO) + t * p.N;
-    S m, r, first = 0, second = 0;
+    S m, r;
     norm_long_stats<T, V>(row, p.N, (S)p.eps, lds, turn, &m, &r);
     if (p.stat && threadIdx.x == 0) {
       static_cast<S*>(p.stat)[2 * t] = m;
       static_cast<S*>(p.stat)[2 * t + 1] = r;
     }
+    double firsts = 0, seconds = 0;
     norm_units<V>(p.N, [&](const RowUnit<V>& u) {
       const Pack<T, V> x = load_unit<T, V>(row, u), d = load_unit<T, V>(grad, u);
       const Pack<TW, V> w = load_unit<TW, V>(static_cast<const TW*>(p.W), u);
+      S of = 0, with = 0;
 #pragma unroll
       for (int i = 0; i < V; i++) {
         const S h = (S)d.e[i] * (S)(float)w.e[i];
-        first += i >= u.skip ? h : (S)0;
-        second += i >= u.skip ? h * (((S)x.e[i] - m) * r) : (S)0;
+        of += i >= u.skip ? h : (S)0;
+        with += i >= u.skip ? h * (((S)x.e[i] - m) * r) : (S)0;
       }
+      firsts += of;
+      seconds += with;
     });
-    first = norm_sum<WG_THREADS>(first, lds, turn) / (S)p.N;
-    second = norm_sum<WG_THREADS>(second, lds, turn) / (S)p.N;
+    const S first = (S)(norm_sum<WG_THREADS>(firsts, lds, turn) / p.N), second = (S)(norm_sum<WG_THREADS>(seconds, lds, turn) / p.N);
     norm_units<V>(p.N, [&](const RowUnit<V>& u) {
       const Pack<T, V> x = load_unit<T, V>(row, u), d = load_unit<T, V>(grad, u);
       const Pack<TW, V> w = load_unit<TW, V>(static_cast<const TW*>(p.W), u);

@@ -156,6 +156,21 @@ def test_layer_norm_of_equal_and_of_special_values():
     assert bool(O.isnan().all())
 
 
+def test_layer_norm_of_a_row_of_2_25():
+    """Squares and products of one size: sums of 32 bits along such a row would be off by a part in 2^9.  Along rows beyond registers they are of 64: c = 2^-24 times the 8
+    neighbours that are added first, the mean's, the squares' and the results' roundings."""
+    N, c = 1 << 25, 2.0 ** -24
+    X = torch.full((1, N), 0.55, dtype=F16, device="cuda")
+    X[:, ::2].neg_()
+    W, O = torch.ones(N, dtype=F16, device="cuda"), _nan((1, N), F16)
+    a = float(X[0, 1])
+    tc.tc_layer_norm(X, W, None, O, 0.0)
+    assert float((O[0, 1::2].float() - 1).abs().max()) <= UNIT[F16] + 24 * c and float((O[0, ::2].float() + 1).abs().max()) <= UNIT[F16] + 24 * c
+    dX = _nan((1, N), F16)
+    tc.tc_layer_norm_grad(torch.full_like(X, a), X, W, dX, None, None, None, 0.0)
+    assert float(dX.float().abs().max()) <= 24 * c  # (h equals its mean)
+
+
 def test_layer_norm_without_rows():
     X, W = torch.empty((0, 9), device="cuda"), torch.ones(9, device="cuda")
     tc.tc_layer_norm(X, W, None, X)
