@@ -216,8 +216,8 @@ __global__ __launch_bounds__(WG_THREADS) void route_balanced_kernel(RouteBalance
     }
     int id = -1;
     if (!exact) {
-      // Keys of 32 bits: where the score lies in a window below the largest one, in steps, then the expert, lower numbers first: a maximum names its expert.  Two that follow each
-      // other in one step, one of them beyond the k-th, are told apart by the scores themselves; where these differ, the wavefront chooses again, by them.
+      // Keys of 32 bits: where the score lies in a window below the largest one, in steps, then the expert, lower numbers first: a maximum names its expert.  Chosen ones that follow each
+      // other in one step are told apart by the scores themselves, and so are the last chosen and all that are left in its step; where these differ, the wavefront chooses again, by them.
       double top = c[0];
 #pragma unroll
       for (int v = 1; v < V; v++) top = most64(top, c[v]);
@@ -227,31 +227,37 @@ __global__ __launch_bounds__(WG_THREADS) void route_balanced_kernel(RouteBalance
       unsigned key[V];
 #pragma unroll
       for (int v = 0; v < V; v++) {
-        const double at = __builtin_fma(c[v], per, from);  // (1 .. steps)
-        key[v] = c[v] == -__builtin_inf() ? 0 : (unsigned)most64(at, 1.0) << number_bits | (last - (lane * V + v));
+        // (1 .. steps: below the window, and beyond `steps` where a bias takes the bits that `from` has, one step holds many)
+        const double at = __builtin_fmin(most64(__builtin_fma(c[v], per, from), 1.0), (double)steps);
+        key[v] = c[v] == -__builtin_inf() ? 0 : (unsigned)at << number_bits | (last - (lane * V + v));
       }
+      const auto score = [&](unsigned of) {  // of the expert that a key names, in all lanes
+        double c_ = -__builtin_inf();
+        const int e = (int)(last - (of & last));
+#pragma unroll
+        for (int v = 0; v < V; v++) c_ = lane * V + v == e ? c[v] : c_;
+        return group_all<G>(c_, most64);
+      };
       unsigned before = 0;
-      for (int i = 0; i <= p.k; i++) {
+      for (int i = 0; i < p.k; i++) {
         unsigned best = key[0];
 #pragma unroll
         for (int v = 1; v < V; v++) best = larger(best, key[v]);
         best = group_all<G>(best, larger);
-        if (best >> number_bits == before >> number_bits && best) {
-          double mine = -__builtin_inf(), other = -__builtin_inf();
-          const int e = (int)(last - (best & last)), f = (int)(last - (before & last));
-#pragma unroll
-          for (int v = 0; v < V; v++) {
-            mine = lane * V + v == e ? c[v] : mine;
-            other = lane * V + v == f ? c[v] : other;
-          }
-          exact |= group_all<G>(mine, most64) != group_all<G>(other, most64);
-        }
+        if (best >> number_bits == before >> number_bits && best) exact |= score(best) != score(before);
         if (lane == i && best) id = (int)(last - (best & last));
         before = best;
 #pragma unroll
         for (int v = 0; v < V; v++) key[v] = key[v] == best ? 0 : key[v];
       }
-      if (lane >= p.k) id = -1;
+      bool near = false;
+#pragma unroll
+      for (int v = 0; v < V; v++) near |= key[v] && key[v] >> number_bits == before >> number_bits;
+      if (__ballot(near)) {
+        const double border = score(before);
+#pragma unroll
+        for (int v = 0; v < V; v++) exact |= key[v] && key[v] >> number_bits == before >> number_bits && c[v] != border;
+      }
       exact = __ballot(exact) != 0;
     }
     if (exact) {

@@ -258,6 +258,35 @@ def test_route_balanced_tells_scores_apart_that_agree_in_32_bits():
     assert len(set(_np(out[1])[0])) == 8
 
 
+@pytest.mark.parametrize("sigmoid", [True, False])
+@pytest.mark.parametrize("E,k,groups,keep", [(256, 4, 1, 1), (256, 4, 16, 9), (30, 4, 1, 1), (300, 20, 1, 1), (64, 1, 1, 1)])
+def test_route_balanced_finds_a_larger_score_behind_equal_ones(sigmoid, E, k, groups, keep):
+    """Scores far below the largest, most of them equal, one of a late expert larger by less than a part in 2^28 of the largest."""
+    T = 40
+    L = torch.full((T, E), -20.0, device="cuda")
+    L[:, 0] = _rand((T,), F32, 5).abs()
+    for t in range(T):
+        L[t, E - 1 - t % 7] = -20.0 + 0.125 * (t % 9)
+        L[t, E // 2] = -20.0 + 0.25 * (t % 5)
+    _check_route(L, None, k, groups, keep, sigmoid, False)
+    _check_route(L[:, 1:].contiguous() if groups == 1 else L, None, k, groups, keep, sigmoid, False)
+
+
+@pytest.mark.parametrize("sigmoid", [True, False])
+@pytest.mark.parametrize("E,k,groups,keep", [(2, 1, 1, 1), (8, 3, 1, 1), (8, 3, 4, 2), (100, 5, 10, 3), (256, 8, 16, 5), (600, 20, 1, 1)])
+def test_route_balanced_of_biases_far_beyond_the_scores(sigmoid, E, k, groups, keep):
+    """An expert that every token shall have, one that none shall have: the order stays that of the formula, whatever the biases' size."""
+    L = _rand((50, E), F32, E, 2.0)
+    for high in (3.0, 3.0e6, 1.7e9, 2.9e15, 1.0e30, torch.finfo(F32).max):
+        for at in ([E - 1], [0], [E // 2, E // 3], []):
+            for low in (0.0, -high):
+                Bias = _rand((E,), F32, 7, 0.1)
+                Bias[E // 4] = low
+                Bias[at] = high
+                _check_route(L, Bias, k, groups, keep, sigmoid, True)
+    _check_route(L, torch.full((E,), -3.0e9, device="cuda"), k, groups, keep, sigmoid, True)
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("sigmoid", [False, True])
 @pytest.mark.parametrize("norm", [False, True])
