@@ -51,6 +51,23 @@ TIMES = [
 ]
 
 
+# the same with sets of operands in turn, so that they come from memory
+TIMES += [
+    (0, 2000, 4, 512, 512, None, 6.0, 8.0, 15.8), (0, 2048, 32, 2048, 1024, None, 24.3, 26.9, 27.6), (0, 512, 1, 4096, 4096, None, 21.1, 26.7, 54.6),
+    (0, 2048, 8, 2048, 2048, None, 33.4, 25.0, 36.4), (0, 8192, 16, 1024, 1024, None, 29.1, 25.7, 23.7), (0, 8192, 128, 1024, 1024, None, 45.1, 47.7, 58.0),
+    (0, 700, 1, 3000, 1000, None, 9.1, 11.0, 21.4), (0, 4096, 4, 1024, 4096, None, 50.0, 37.5, 60.7), (0, 8192, 32, 1024, 2048, None, 51.4, 43.7, 38.3),
+    (0, 2048, 1, 2048, 2048, None, 16.0, 16.9, 32.4), (0, 8192, 1, 1024, 4096, None, 63.1, 41.9, 60.7), (0, 16384, 32, 2048, 4096, None, 276.8, 195.0, 194.7),
+    (0, 16384, 32, 4096, 2048, None, 293.7, 211.2, 184.0), (0, 32768, 32, 2048, 4096, None, 501.3, 349.6, 312.9), (0, 65536, 32, 2048, 4096, None, 936.4, 651.7, 560.8),
+    (0, 16384, 16, 2048, 4096, None, 259.4, 190.7, 185.8), (0, 16384, 8, 2048, 4096, None, 241.3, 174.2, 178.7), (0, 8192, 4, 4096, 4096, None, 239.1, 174.2, 178.4),
+    (0, 8192, 16, 4096, 2048, None, 151.4, 111.2, 106.8), (0, 16384, 64, 2048, 2048, None, 173.3, 134.6, 113.7), (0, 8192, 8, 1024, 4096, None, 79.8, 65.2, 62.4),
+    (0, 4096, 1, 8192, 4096, None, 242.1, 165.9, 132.2), (0, 8192, 1, 8192, 8192, None, 847.5, 591.9, 460.9), (0, 4096, 1, 8192, 1024, None, 66.2, 48.7, 49.5),
+    (0, 4096, 64, 1024, 1024, None, 26.4, 29.4, 29.2), (0, 4096, 16, 2048, 2048, None, 51.3, 43.5, 38.0), (0, 2048, 16, 2048, 2048, None, 35.3, 26.2, 37.0),
+    (0, 16384, 128, 2048, 1024, None, 133.2, 102.9, 123.9), (0, 32768, 128, 1024, 2048, None, 184.7, 135.5, 119.7), (0, 1024, 1, 4096, 4096, None, 27.1, 28.0, 54.7),
+    (0, 4096, 8, 4096, 4096, None, 151.5, 116.2, 122.8), (0, 2048, 1, 4096, 4096, None, 63.5, 41.5, 60.9), (0, 1500, 1, 8192, 4096, None, 86.1, 74.8, 63.0),
+    (0, 3000, 1, 4096, 8192, None, 156.6, 120.3, 110.4), (0, 65536, 64, 1024, 2048, None, 292.2, 204.5, 182.7),
+]
+
+
 @pytest.mark.parametrize("f32,R,E,N,K,few,t64,t128,t256", TIMES)
 def test_the_choice_is_near_the_best(kernel, f32, R, E, N, K, few, t64, t128, t256):
     us = {0: few, 64: t64, 128: t128, 256: t256}
