@@ -581,7 +581,8 @@ tc_status tc_expert_sum_grad(const void *dO, const void *Y, const float *Wt,
  * X's type or fp32 (weight_type).  eps >= 0 (TC_ERR_SHAPE otherwise; 0 gives NaN for a
  * row of equal values, as the formula has).  N below 2^26.  The squares are taken of the
  * differences to the mean, not of the values.  Sums in fp64 for fp32 rows and along rows of more
- * than 8192 elements, else in fp32.
+ * than 8192 elements, else in fp32: squares of bf16 rows are in fp32, Inf for differences from 2^64 on
+ * (then O = B).
  */
 tc_status tc_layer_norm(const void *X, const void *W, const void *B, void *O,
                         int64_t T, int64_t N, float eps, tc_type type,

@@ -58,9 +58,17 @@ __device__ __forceinline__ int offset_within(const int* off, int g, int R) { ret
 // Workgroup `bid`'s tile, or false.  Tiles of one expert follow each
 // other in blocks of 8 row tiles by all column tiles, row tiles first, so that workgroups that run together share operands; and every
 // XCD (workgroups equal modulo 8) takes a run of its own.  One round trip to memory for up to 63 experts.
-__device__ __forceinline__ bool expert_tile(const int* off, int E, int R, int bm, int nt, unsigned bid, ExpertTile* t) {
+// KIND: which row tiles count.  *run (where given): the workgroups of an XCD.
+enum { TILES_ALL, TILES_FULL, TILES_SHORT };  // SHORT: an expert's last one where it has bm/2 rows or fewer; FULL: the others
+template <int KIND = TILES_ALL>
+__device__ __forceinline__ bool expert_tile(const int* off, int E, int R, int bm, int nt, unsigned bid, ExpertTile* t, unsigned* run_ = nullptr) {
   const int lane = threadIdx.x & 63;
   int lo, hi;
+  const auto counted = [&](int rows) {
+    if constexpr (KIND == TILES_ALL) return (rows + bm - 1) / bm;
+    else if constexpr (KIND == TILES_FULL) return (rows + bm / 2 - 1) / bm;
+    else return (rows + bm - 1) / bm - (rows + bm / 2 - 1) / bm;
+  };
   const auto tiles = [&](int g, int* reached) {  // of expert g; its rows go to lo, hi; reached: by the experts before this lane 0's, then before the next one's
     lo = hi = R;
     if (g <= E) {
@@ -79,7 +87,7 @@ __device__ __forceinline__ bool expert_tile(const int* off, int E, int R, int bm
       if (lane) lo = before;
     }
     *reached = __shfl(hi, 63);
-    return (unsigned)((hi - lo + bm - 1) / bm) * nt;
+    return (unsigned)counted(hi - lo) * nt;
   };
   const auto up_to = [&](unsigned n) {  // inclusive sums over the lanes
 #pragma unroll
@@ -93,6 +101,7 @@ __device__ __forceinline__ bool expert_tile(const int* off, int E, int R, int bm
   unsigned n = tiles(lane, &reached), incl = up_to(n), total = __shfl(incl, 63);
   for (int base = 64; base <= E; base += 64) total += __shfl(up_to(tiles(base + lane, &reached)), 63);
   const unsigned run = (total + 7) / 8;
+  if (run_) *run_ = run;
   if (bid / 8 >= run) return false;
   const unsigned at = (bid & 7) * run + bid / 8;
   if (at >= total) return false;
@@ -110,11 +119,12 @@ __device__ __forceinline__ bool expert_tile(const int* off, int E, int R, int bm
       t->e = base + src;
       t->lo = __shfl(lo, src);
       t->hi = __shfl(hi, src);
-      const int mt = (t->hi - t->lo + bm - 1) / bm;
+      const int mt = counted(t->hi - t->lo);
       const int block = (int)(local / (unsigned)(8 * nt)), in = (int)(local % (unsigned)(8 * nt));
       const int rows = min(8, mt - 8 * block);
       t->m = 8 * block + in % rows;
       t->n = in / rows;
+      if (KIND == TILES_SHORT) t->m = (t->hi - t->lo) / bm;
       return true;
     }
     before += __shfl(incl, 63);

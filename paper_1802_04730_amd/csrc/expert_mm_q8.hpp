@@ -14,7 +14,7 @@
 // values, widened, and sums them in 32 bits.
 //
 // Measured, rows and weights in 8 bits, bfloat16: (R,N,K) = (4096,8192,4096) 125-131 us (2.1-2.2 PFLOP/s; the library's product without blocks 95), 8192^3 460 (2.4), (4096,4096,8192) 109
-// (2.5); 32 experts, 16384 rows, uneven shares, 2048 x 4096 203, the gradient of the rows with a gate 223; eight experts with 4 rows each, 4096 x 2048, 14 (4.8 TB/s of weights).  A stage of a tile
+// (2.5); 32 experts, 16384 rows, uneven shares, 2048 x 4096 187-206, the gradient of the rows with a gate 213-230; eight experts with 4 rows each, 4096 x 2048, 14 (4.8 TB/s of weights).  A stage of a tile
 // of 256 takes 1.4 us where few tiles run and 1.5-1.7 where all do; its products alone 0.87, or 1.2 at the power that 256 compute units may draw.  What is left are the loads: 0.3 us a stage,
 // as four wavefronts ask the address path at once, whether LDS is read or not, and 0.1 for two barriers.  Tried and left: a branch behind each matrix instruction that gives every wavefront slots of its
 // own for its loads (2.6 us a stage), a copy of the loop for each wavefront instead (1.6), eight wavefronts (1.4 / 1.7), loads spread over the next stage's first steps too (1.5 / 1.7), buffer
@@ -120,21 +120,22 @@ constexpr int Q8_CHUNK = 64;  // stages whose scales are in LDS
 // stands still where the address path has more than it takes.  Before the last step another barrier: the next stage, requested a stage and a half before, is in LDS, and the
 // last step replaces each column's fragment by the next stage's as soon as it is used.  Four wavefronts: 128 x 128 of a tile of 256 each read a third less from LDS (128 KB a
 // stage) than eight, whose reads and the loads' writes would take as long as the products; a wavefront has all 512 registers of its SIMD's lanes, half of them sums.
+// LDS of a tile: two stages and the scales, or the results on their way out.
+template <typename T, int BM, int BN>
+constexpr int q8_tile_lds() {
+  constexpr int in = 2 * (BM + BN) * EMM_STAGE + Q8_CHUNK * (BM + (BN + Q8_BLOCK - 1) / Q8_BLOCK), out = BM * BN * sizeof(T);
+  return in > out ? in : out;
+}
+// Rows from m0 on (BM of them, or up to `hi`), BN columns from n0 on.
 template <typename T, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__(64 * WM * WN) void expert_mm_q8_kernel(Q8Args p) {
+__device__ __forceinline__ void q8_tile_product(const Q8Args& p, char* lds, int e, int m0, int hi, int n0) {
   constexpr int NW = WM * WN, MI = BM / WM / 16, NI = BN / WN / 16;
   constexpr int PA = BM / 8 / NW, PB = BN / 8 / NW, LOADS = PA + PB;  // loads of a wavefront a stage, 8 rows each
   constexpr int EACH = LOADS / (MI / 2);                              // of them in each of the steps of a stage's second half
   constexpr int BLOCKS = (BN + Q8_BLOCK - 1) / Q8_BLOCK;
   static_assert(MI % 2 == 0 && EACH * (MI / 2) == LOADS && PA * 8 * NW == BM && PB * 8 * NW == BN && BN / WN <= Q8_BLOCK, "whole steps, loads and blocks");
   constexpr int BYTES_A = BM * EMM_STAGE, STAGE = (BM + BN) * EMM_STAGE;
-  constexpr int SCALES = Q8_CHUNK * (BM + BLOCKS), OUT = BM * BN * sizeof(T);
-  __shared__ __align__(16) char lds[2 * STAGE + SCALES > OUT ? 2 * STAGE + SCALES : OUT];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, q = lane >> 4;
-  ExpertTile t;
-  if (!q8_tile(p, BM, &t)) return;
-  const int lo = __builtin_amdgcn_readfirstlane(t.lo), hi = __builtin_amdgcn_readfirstlane(t.hi), e = __builtin_amdgcn_readfirstlane(t.e);
-  const int m0 = lo + __builtin_amdgcn_readfirstlane(t.m) * BM, n0 = __builtin_amdgcn_readfirstlane(t.n) * BN;
   const int rm = (wave / WN) * (BM / WM), cn = (wave % WN) * (BN / WN);
   const bool owned = e < p.E && p.T > 0;
   f4 acc[MI][NI];
@@ -348,6 +349,29 @@ __global__ __launch_bounds__(64 * WM * WN) void expert_mm_q8_kernel(Q8Args p) {
         if (y < left) out[y] = v[y];
     }
   }
+}
+
+// A tile of 256 whose expert has 128 rows or fewer left, as every other one has, takes a tile of 128 x 256 instead (0.58 of its time), and these come after the whole ones:
+// an XCD's compute units start on them as they get free, not on a last whole tile each.  Uneven shares, (E,R,N,K), us, before and after: (32,16384,4096,2048) 202 and 187,
+// (8,16384,2048,4096) 178 and 165, (32,32768,2048,4096) 319 and 302, (64,16384,2048,2048) 114 both; in the order of the experts 202, 178, 316, 115.
+template <typename T, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(64 * WM * WN) void expert_mm_q8_kernel(Q8Args p) {
+  __shared__ __align__(16) char lds[q8_tile_lds<T, BM, BN>()];
+  ExpertTile t;
+  if (BM == 256 && p.off) {
+    unsigned run;
+    if (!expert_tile<TILES_FULL>(p.off, p.E, p.R, BM, p.nt, blockIdx.x, &t, &run) &&
+        (blockIdx.x / 8 < run || !expert_tile<TILES_SHORT>(p.off, p.E, p.R, BM, p.nt, blockIdx.x - 8 * run, &t)))
+      return;
+  } else if (!q8_tile(p, BM, &t)) {
+    return;
+  }
+  const int lo = __builtin_amdgcn_readfirstlane(t.lo), hi = __builtin_amdgcn_readfirstlane(t.hi), e = __builtin_amdgcn_readfirstlane(t.e);
+  const int m0 = lo + __builtin_amdgcn_readfirstlane(t.m) * BM, n0 = __builtin_amdgcn_readfirstlane(t.n) * BN;
+  if constexpr (BM == 256) {
+    if (hi - m0 <= BM / 2) return q8_tile_product<T, BM / 2, BN, WM, WN>(p, lds, e, m0, hi, n0);
+  }
+  q8_tile_product<T, BM, BN, WM, WN>(p, lds, e, m0, hi, n0);
 }
 
 // Few rows an expert (a decoding step): 16 rows by 16 CT columns a workgroup, whose wavefronts share the reduction; operands go from memory to registers in the

@@ -121,7 +121,7 @@ tc_status quantize_rows(const void* X, void* Q, void* S, int64_t R, int64_t K, t
 template <typename T, int BM, int WM, int WN>
 tc_status launch_q8_tile(Q8Args a, hipStream_t s) {
   a.nt = (int)ceil_div(a.NO, BM);
-  const int64_t grid = (most_row_tiles(a.R, a.E, BM) * a.nt + 7) / 8 * 8;
+  const int64_t grid = (most_row_tiles(a.R, a.E, BM) * a.nt + 7) / 8 * 8 + (BM == 256 ? 8 : 0);  // (two sets of tiles, each in whole eights)
   if (grid > kMostIndex / (64 * WM * WN) * 2) return TC_ERR_UNSUPPORTED;
   expert_mm_q8_kernel<T, BM, BM, WM, WN><<<dim3((unsigned)grid), dim3(64 * WM * WN), 0, s>>>(a);
   return launched();

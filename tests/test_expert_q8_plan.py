@@ -27,6 +27,7 @@ def kernel(tmp_path_factory):
 def test_every_kernel_is_tested(kernel):
     for side, f32, T, R, E, N, K in big.SHAPES:
         assert kernel(f32, R, E, N, K) == side
+    assert {kernel(0, *shape) for shape in big.SHORT} == {256}
     taken = {kernel(f32, R, E, N, K) for T, R, E, N, K in small.MM_SHAPES for f32 in (0, 1)}
     assert {0, 64} <= taken
 

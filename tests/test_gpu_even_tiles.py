@@ -65,6 +65,45 @@ def test_large_tiles_and_long_reductions(dtype, T, R, E, N, K):
         assert torch.equal(dX, _product(dY, W.transpose(1, 2), Off, None, R).float().to(dtype))
 
 
+SHORT = [(9000, 7, 8200, 1000), (9000, 6, 8185, 300), (20000, 70, 4100, 520), (70000, 300, 1000, 650)]  # R, E, N, K
+
+
+def _odd_shares(R, E, seed):
+    """Offsets that leave last row tiles of a tile of 256 of every kind, rows before the first expert and behind the last."""
+    rng = np.random.default_rng(seed)
+    rest, off = rng.permutation(np.resize([1, 128, 0, 129, 256, 127, 255], E)), [3]
+    for i, r in enumerate(rest):
+        spare = (R - 40 - off[-1] - int(rest[i:].sum())) // 256
+        off.append(off[-1] + int(r) + 256 * (min(spare, int(rng.integers(0, 2 * (R // 256) // E + 1))) if r or i % 2 else 0))
+    assert off[-1] < R - 30
+    return np.array(off)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("R,E,N,K", SHORT)
+def test_last_row_tiles_of_every_kind(dtype, R, E, N, K):
+    rng = np.random.default_rng(R + K)
+    T = R // 2
+    X, W = _whole((T, K), 1, dtype, (T,)), _whole((E, N, K), 2, dtype, (E, -(-N // 128)))
+    Q, S, _, _ = _weights8(W)
+    ws = _bytes(tc.tc_expert_mm_q8_workspace_bytes(T, R, E, N, K))
+    Row, gate = _ints(rng.integers(-1, T + 1, R)), _whole((R, N), 3, dtype, (R,))
+    for seed, gated in ((1, False), (2, True)):
+        Off = _odd_shares(R, E, seed)
+        Y = _nan((R, N), dtype)
+        tc.tc_expert_mm_q8(X, None, Q, S, _ints(Off), Row, gate if gated else None, Y, ws)
+        want = _product(X, W, Off, Row, R)
+        want = torch.where(gate > 0, want, 0.0) if gated else want
+        assert torch.equal(Y[Off[0]:], want[Off[0]:].float().to(dtype))
+        assert bool(Y[:Off[0]].isnan().all())
+    for off in (np.full(E + 1, 0), np.full(E + 1, R), np.r_[np.zeros(E), R], np.r_[0, np.full(E, R)], np.r_[np.linspace(R, 0, E), 2 ** 31 - 1], np.r_[-5, rng.integers(-R, 2 * R, E)]):
+        big = torch.full((R + 64, N), 7.0, dtype=dtype, device="cuda")
+        tc.tc_expert_mm_q8(X, None, Q, S, _ints(np.asarray(off, np.int64).clip(-2 ** 31, 2 ** 31 - 1)), Row, None, big[:R], ws)
+        reached = np.maximum.accumulate(np.clip(off, 0, R)).astype(np.int64)
+        want = _product(X, W, reached, Row, R)
+        assert torch.equal(big[reached[0]:R], want[reached[0]:].float().to(dtype)) and bool((big[R:] == 7.0).all()) and bool((big[:reached[0]] == 7.0).all())
+
+
 def test_a_layer_of_experts_in_large_tiles_is_the_same_each_time():
     """No wait between stages may be missing: the same bits over many calls, between calls of other sizes."""
     T, E, N, K = 8192, 1, 8192, 3300
