@@ -7,10 +7,11 @@ namespace tc355 {
 // Side of the (square) tile: the estimate is a compute unit's number of tiles times a tile's products, over the rate that the side reaches relative to the others, and as
 // many stages more as a tile's start and end take.  float outputs (by the half instruction) take 128 at most.  The rates are those of operands that come from memory, not from the
 // caches that the product before left them in: tiles of 128, two a compute unit, ask for a third more of them at a time and lose most.  Measured so (sets of operands in turn),
-// bfloat16, us, sides 64 / 128 / 256: (E,R,N,K) = (1,4096,8192,4096) 242 / 166 / 132, 8192^3 848 / 592 / 461, of (1,4096,8192,1024) 66 / 49 / 50, uneven shares (32,16384,2048,4096)
-// 277 / 195 / 195, even ones 265 / 179 / 139, uneven (32,16384,4096,2048) 294 / 211 / 184, (8,16384,2048,4096) 241 / 174 / 179, (16,16384,2048,4096) 259 / 191 / 186, (64,16384,2048,2048)
-// 173 / 135 / 114, (128,32768,1024,2048) 185 / 136 / 120, (128,16384,2048,1024) 133 / 103 / 124, (8,4096,4096,4096) 152 / 116 / 123, (16,2048,2048,2048) 35 / 26 / 37, (64,2048,1024,2048) 41 / 34 / 43,
-// (1,512,4096,4096) 21 / 27 / 55, (4,2000,512,512) 6.0 / 8.0 / 16; float, sides 64 / 128, from the caches: (1,4096,4096,4096) 216 / 183, (32,8192,2048,2048) 146 / 128, (16,2048,2048,2048) 39 / 47,
+// bfloat16, us, sides 64 / 128 / 256: (E,R,N,K) = (1,4096,8192,4096) 241 / 166 / 131, 8192^3 839 / 580 / 456, of (1,4096,8192,1024) 66 / 47 / 49, uneven shares (32,16384,2048,4096)
+// 276 / 195 / 180, even ones 264 / 178 / 136, uneven (32,16384,4096,2048) 293 / 211 / 183, (8,16384,2048,4096) 240 / 173 / 159, (16,16384,2048,4096) 256 / 191 / 168, (64,16384,2048,2048)
+// 173 / 133 / 113, (128,32768,1024,2048) 186 / 134 / 116, (128,16384,2048,1024) 133 / 103 / 106, (8,4096,4096,4096) 152 / 115 / 106, (16,2048,2048,2048) 35 / 26 / 37, (64,2048,1024,2048) 41 / 34 / 39,
+// (256,16384,1024,2048) 151 / 136 / 153, (1,512,4096,4096) 21 / 27 / 54, (4,2000,512,512) 6.1 / 8.0 / 16.  Over 41 shapes the choice is 2.2 % off the best side; at worst 15 %, where an expert's few rows
+// make short tiles of 256, which the estimate counts as half lost: (16,4096,2048,2048) 51 / 43 / 38, (32,8192,1024,2048) 51 / 44 / 38, taken 128.  float, sides 64 / 128, from the caches: (1,4096,4096,4096) 216 / 183, (32,8192,2048,2048) 146 / 128, (16,2048,2048,2048) 39 / 47,
 // (12,2100,1001,517) 12 / 17.
 inline int q8_tile_side(bool f32, int cus, int64_t R, int64_t E, int64_t NO, int64_t stages) {
   const struct {
