@@ -15,7 +15,8 @@
 // 2^18 elements of one: in 32 bits, squares of one size would be off by parts in 2^8.
 //
 // Measured: 16384 rows of 4096 bfloat16, weights in float, 51-53 us (5.1-5.2 TB/s) forward, 87-92 for the gradient (4.6) and 6.5 for its join; 8 rows of 2048 4.2; 1500 rows of 333 floats
-// 3.8, 7.9 and 4.5 (16 rows a part, four a group of lanes: 10.5 and 3).
+// 3.8, 7.9 and 4.5 (16 rows a part, four a group of lanes: 10.5 and 3).  Widths of four units a lane, 16384 rows of bfloat16: 2048 30 forward and 77 for gradient and join (2.6 TB/s), 5120 65 and 166 (3.0), 8192 97 and 193 (4.2): the
+// gradient's sums take 270 registers there, one wavefront a SIMD.  Beyond registers: 8192 rows of 8192 floats 158 (3.4 TB/s, each row read three times, mostly from cache) and 399 (2.0), of 12288 bfloat16 161 and 409.
 #pragma once
 #include "expert_types.hpp"
 #include "lanes.hpp"

@@ -14,7 +14,8 @@
 // chosen are computed again by the lanes that write them, all at once.  What bounds it is the rounds' latency and the exponentials of 64 bits.
 //
 // Measured: 16384 tokens of 256 experts, 16 groups of which 5, 8 chosen, 28-32 us for the selection (43 with k rounds over keys of 64 bits, library exponentials and scores at a stride of
-// 128 bytes in LDS; of it 8 for the rounds, 3 for the groups), 12 for sums and places, 7-8 for the gradient; tc_route, with as many lanes a token, takes 48 for all but the gradient.
+// 128 bytes in LDS; of it 8 for the rounds, 3 for the groups), 12 for sums and places, 7-8 for the gradient.  All but the gradient 37, by softmax without groups 31; tc_route, which gives as many
+// experts 64 lanes a token, 44.
 // 16 tokens of 128, 8 groups of which 3, 6 chosen, 9.7 in one launch (7.4 with one chosen and no groups).
 #pragma once
 #include "expert_types.hpp"
@@ -306,7 +307,8 @@ struct RouteBalancedGradArgs {
   int sigmoid;
 };
 
-// The chosen experts' part in 64 bits, by the lanes that hold the slots: their scores may be far below the others'.
+// The chosen experts' part in 64 bits, by the lanes that hold the slots: their scores may be far below the others'.  softmax's other columns and its sum take
+// exponentials in 32 bits (the sum joins lanes in 64): such a column is off by some 2^-18 of itself, in float too, which a gradient bears; in 64 bits they would cost what they cost the selection.
 template <typename T, int G, int V>
 __global__ __launch_bounds__(WG_THREADS) void route_balanced_grad_kernel(RouteBalancedGradArgs a, int64_t first) {
   const RouteGradArgs& p = a.r;

@@ -62,7 +62,9 @@ tc_status by_norm_types(tc_type type, tc_type weight, F f) {
   return by_type(type, [&](auto t) { return weight == TC_F32 ? f(t, float{}) : f(t, t); });
 }
 
-// Parts of the sums for dW and dB.
+// Parts of the sums for dW and dB: a row each while there are few, so that as many compute units work on them, though each part's sums are written and read again (N of 4 or 8 bytes for dW, as many for dB).  Measured, the
+// gradient with its join, us, a row a part / 16 rows: bfloat16 (T,N) = (128,4096) 12 / 31, (512,2048) 20 / 24, (512,4096) 26 / 31, (512,8192) 44 / 51, (2048,4096) 29 / 34; float (300,1000) 13 / 17, (1500,333) 13 / 13.  The other
+// way round where a part has the most to write beside its rows: bfloat16 (2048,2048) 39 / 28, (2048,8192) 58 / 54, float beyond registers (512,8192) 61 / 37.  From 8192 rows on both are 512.
 int64_t norm_parts(int64_t T) { return std::min<int64_t>(T, NORM_MOST_PARTS); }
 struct NormPlan {
   int64_t parts, stat, bytes;
